@@ -88,7 +88,7 @@ enum {
   BIGMAC_ERR_WORKSPACE = -2,
   BIGMAC_ERR_UNSUPPORTED = -3,
   BIGMAC_ERR_HIP = -4,
-  BIGMAC_ERR_TOO_LARGE = -5   /* bigmac_dispatch_static: the problem exceeds the library's static scratch */
+  BIGMAC_ERR_TOO_LARGE = -5   /* a size beyond a stated limit (bigmac_dispatch_static: the library's static scratch) */
 };
 
 typedef struct {
@@ -297,6 +297,61 @@ int bigmac_expert_pairing(const bigmac_dims *dims, int training);
  * only, or nothing.  For measurement code, like the calls above.  training: 0 = a call with saved ==
  * NULL.  Negative: an error code for bad dims. */
 int bigmac_topk_folding(const bigmac_dims *dims, int training);
+
+/* ------------------------------------------------------------------ the norms around a block ---
+ * A transformer block puts the layer between two norms, scales what comes back and adds it to the
+ * residual stream.  One call does what lies between two blocks, row by row (T rows of d columns):
+ *     z = alpha x + g n_post(y)      x: the residual stream, y: what the block returned (norm behind it, its gate, residual scale)
+ *     u = n_pre(z)                   what the next block reads (norm in front of it)
+ *     n(v) = w (v - m) / sqrt(mean((v - m)^2) + eps) + b,   m = mean(v) (BIGMAC_NORM_LAYER) or 0 (BIGMAC_NORM_RMS)
+ * With BIGMAC_NORM_PRE alone there is no branch: u = n_pre(x).  With BIGMAC_NORM_POST alone u is not made.
+ * u is the norm of z as it is stored (rounded to x_dtype), so that the backward, which reads z, sees the same rows.
+ * Statistics and sums are fp32; a layer norm's variance is taken behind its mean. */
+typedef enum { BIGMAC_NORM_RMS = 0, BIGMAC_NORM_LAYER = 1 } bigmac_norm_kind;
+typedef enum {
+  BIGMAC_GATE_NONE = 0,    /* g = 1                                                              */
+  BIGMAC_GATE_CHANNEL = 1, /* g[d] fp32: one value per column, shared by all rows                */
+  BIGMAC_GATE_TOKEN = 2,   /* g[T] fp32: one value per row                                       */
+  BIGMAC_GATE_FULL = 3     /* g[T, d] of u_dtype                                                 */
+} bigmac_gate;
+enum {
+  BIGMAC_NORM_POST = 1,       /* parts: y, its norm, the gate and the residual                   */
+  BIGMAC_NORM_PRE = 2,        /*        the norm that makes u                                    */
+  BIGMAC_NORM_ACCUMULATE = 4  /* backward: add to d_post_w, d_post_b, d_pre_w, d_pre_b and a channel gate's gradient (else overwrite) */
+};
+
+typedef struct {
+  int32_t T, d;      /* rows (1 .. 2^30), columns (a multiple of 8, 8 .. 8192; past either BIGMAC_ERR_TOO_LARGE) */
+  int32_t x_dtype;   /* the residual stream: x, z, dz, dx                                        */
+  int32_t y_dtype;   /* what a block's calls return: y and du (bigmac_layer_forward's y, bigmac_layer_backward's dx) */
+  int32_t u_dtype;   /* what a block's calls read: u, dy, a full gate and its gradient           */
+  int32_t kind, parts, gate;
+  float eps, alpha;  /* alpha: 1 without BIGMAC_NORM_POST                                        */
+} bigmac_norm_dims;
+
+typedef struct {     /* caller-owned, never written.  Weights are required for the parts that are there and NULL for the others; biases may be NULL */
+  const float *post_w, *post_b; /* [d] fp32                                                      */
+  const float *pre_w, *pre_b;   /* [d] fp32                                                      */
+  const void *gate;             /* by `gate`                                                     */
+} bigmac_norm_params;
+
+/* Base pointers 16-byte aligned (BIGMAC_ERR_INVALID_ARG else).  y and z with BIGMAC_NORM_POST, u with BIGMAC_NORM_PRE,
+ * NULL without.  z may be x (in place). */
+int bigmac_norm_forward(const bigmac_norm_dims *dims, const bigmac_norm_params *params, const void *x, const void *y,
+                        void *z, void *u, void *stream);
+
+/* Bytes of workspace of bigmac_norm_backward (0 if the dims are invalid).  Host only. */
+size_t bigmac_norm_workspace_bytes(const bigmac_norm_dims *dims);
+
+/* Gradients, from what the forward read and wrote.  dz: the gradient of z that comes along the residual stream (may be NULL
+ * with BIGMAC_NORM_PRE: none); du: that of u.  With dZ = dz + (gradient of n_pre)(du):
+ *     dx = alpha dZ,   dy = (gradient of n_post)(g dZ),   d_gate = dZ n_post(y), summed over what g is shared by.
+ * z (x of a call without BIGMAC_NORM_POST), du, d_pre_w with BIGMAC_NORM_PRE and y, dy, d_post_w with BIGMAC_NORM_POST, NULL
+ * without; d_post_b, d_pre_b, d_gate exactly where params has post_b, pre_b, gate.  dx may be dz (in place).  The sums over
+ * rows run in a fixed order: equal inputs give equal bits. */
+int bigmac_norm_backward(const bigmac_norm_dims *dims, const bigmac_norm_params *params, const void *z, const void *y,
+                         const void *du, const void *dz, void *dx, void *dy, void *d_gate, float *d_post_w,
+                         float *d_post_b, float *d_pre_w, float *d_pre_b, void *ws, size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

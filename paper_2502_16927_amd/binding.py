@@ -14,6 +14,9 @@ F32, BF16 = 0, 1
 ORDER_DCCA, ORDER_CDAC = 0, 1
 FLAG_ACCUMULATE, FLAG_OUT_BF16, FLAG_WIRE_BF16, FLAG_TILES_LARGE, FLAG_TILES_SMALL, FLAG_ROUTE_LOW, FLAG_NO_FUSED_DISPATCH = 1, 2, 4, 8, 16, 32, 64
 WS_ROUTE, WS_DISPATCH, WS_GROUPED_FFN, WS_LAYER_FORWARD, WS_LAYER_TRAIN, WS_SAVED, WS_AUX_LOSS = range(7)
+NORM_RMS, NORM_LAYER = 0, 1
+GATE_NONE, GATE_CHANNEL, GATE_TOKEN, GATE_FULL = range(4)
+NORM_POST, NORM_PRE, NORM_ACCUMULATE = 1, 2, 4
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libbigmac.so")
 _lib = None
@@ -26,6 +29,15 @@ class Dims(ctypes.Structure):
 
 class Params(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("w_down", "w_up", "w_gate", "gate_bias", "w1", "w2", "b1", "b2")]
+
+
+class NormDims(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("T", "d", "x_dtype", "y_dtype", "u_dtype", "kind", "parts", "gate")] + [
+        (n, ctypes.c_float) for n in ("eps", "alpha")]
+
+
+class NormParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("post_w", "post_b", "pre_w", "pre_b", "gate")]
 
 
 class BigmacError(RuntimeError):
@@ -82,6 +94,13 @@ def lib() -> ctypes.CDLL:
         L.bigmac_stage_name.argtypes = [ci]
         L.bigmac_gather_probe.restype = ci
         L.bigmac_gather_probe.argtypes = [vp, vp, ctypes.c_int64, ctypes.c_int64, ci, vp, vp]
+        np_, pp = ctypes.POINTER(NormDims), ctypes.POINTER(NormParams)
+        L.bigmac_norm_workspace_bytes.restype = sz
+        L.bigmac_norm_workspace_bytes.argtypes = [np_]
+        L.bigmac_norm_forward.restype = ci
+        L.bigmac_norm_forward.argtypes = [np_, pp, vp, vp, vp, vp, vp]
+        L.bigmac_norm_backward.restype = ci
+        L.bigmac_norm_backward.argtypes = [np_, pp] + [vp] * 12 + [sz, vp]
         L.bigmac_mfma_probe.restype = ci
         L.bigmac_mfma_probe.argtypes = [ci, ci, vp, ctypes.POINTER(ctypes.c_double), vp]
         _lib = L
@@ -91,7 +110,7 @@ def lib() -> ctypes.CDLL:
 EXPORTS = ("bigmac_workspace_bytes", "bigmac_status_string", "bigmac_forward_matrix_flops", "bigmac_permute_bytes",
            "bigmac_saved_layout", "bigmac_saved_aux_layout", "bigmac_aux_loss", "bigmac_route", "bigmac_dispatch", "bigmac_dispatch_static", "bigmac_grouped_ffn", "bigmac_combine",
            "bigmac_layer_forward", "bigmac_layer_backward", "bigmac_set_stage_events", "bigmac_stage_name", "bigmac_dispatch_folding", "bigmac_expert_pairing", "bigmac_topk_folding",
-           "bigmac_mfma_probe", "bigmac_gather_probe")
+           "bigmac_mfma_probe", "bigmac_gather_probe", "bigmac_norm_workspace_bytes", "bigmac_norm_forward", "bigmac_norm_backward")
 STAGE_COUNT = 22
 
 
@@ -216,6 +235,28 @@ def bigmac_layer_backward(dims, params, x, dy, saved, dx, d_w_down, d_w_up, d_w_
     _check(lib().bigmac_layer_backward(ctypes.byref(dims), ctypes.byref(params), _ptr(x), _ptr(dy), _ptr(saved), _ptr(dx),
                                        _ptr(d_w_down), _ptr(d_w_up), _ptr(d_w_gate), _ptr(d_w1), _ptr(d_w2), _ptr(d_b1), _ptr(d_b2),
                                        _ptr(ws), _nbytes(ws), _stream(stream)), "bigmac_layer_backward")
+
+
+def make_norm_dims(T, d, x_dtype=BF16, y_dtype=BF16, u_dtype=BF16, kind=NORM_RMS, parts=NORM_POST | NORM_PRE, gate=GATE_NONE, eps=1e-5, alpha=1.0) -> NormDims:
+    return NormDims(T, d, x_dtype, y_dtype, u_dtype, kind, parts, gate, eps, alpha)
+
+
+def make_norm_params(post_w=None, post_b=None, pre_w=None, pre_b=None, gate=None) -> NormParams:
+    return NormParams(_ptr(post_w), _ptr(post_b), _ptr(pre_w), _ptr(pre_b), _ptr(gate))
+
+
+def norm_workspace_bytes(dims: NormDims) -> int:
+    return lib().bigmac_norm_workspace_bytes(ctypes.byref(dims))
+
+
+def bigmac_norm_forward(dims, params, x, y, z, u, stream=None):
+    _check(lib().bigmac_norm_forward(ctypes.byref(dims), ctypes.byref(params), _ptr(x), _ptr(y), _ptr(z), _ptr(u), _stream(stream)), "bigmac_norm_forward")
+
+
+def bigmac_norm_backward(dims, params, z, y, du, dz, dx, dy, d_gate, d_post_w, d_post_b, d_pre_w, d_pre_b, ws, stream=None):
+    _check(lib().bigmac_norm_backward(ctypes.byref(dims), ctypes.byref(params), _ptr(z), _ptr(y), _ptr(du), _ptr(dz), _ptr(dx), _ptr(dy), _ptr(d_gate),
+                                      _ptr(d_post_w), _ptr(d_post_b), _ptr(d_pre_w), _ptr(d_pre_b), _ptr(ws), _nbytes(ws), _stream(stream)),
+           "bigmac_norm_backward")
 
 
 def dispatch_folding(dims, training: bool) -> int:
