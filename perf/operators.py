@@ -195,7 +195,7 @@ def _handles(s):
             s["ws"] = B.alloc_bytes(B.norm_workspace_bytes(s["dims"]), DEV)
     elif c["kind"] == "rows":
         s["codes"] = torch.empty((c["rows"], c["cols"] // 2), dtype=torch.uint8, device=DEV)
-        s["scales"] = torch.empty((c["rows"], c["cols"] // 32), dtype=torch.uint8, device=DEV)
+        s["scales"] = torch.empty((c["rows"], B.mx_scale_bytes(c["cols"])), dtype=torch.uint8, device=DEV)
     elif c["kind"] == "weights":
         s["packed"] = B.alloc_bytes(B.mx_packed_bytes(c["N"], c["n_in"], c["n_out"]), DEV)
     else:
@@ -209,7 +209,7 @@ def _handles(s):
             s["ws"] = B.alloc_bytes(B.workspace_bytes(s["dims"], B.WS_MX_GROUPED_FFN), DEV)
         else:
             s["codes"] = torch.empty((c["rows"], c["n_in"] // 2), dtype=torch.uint8, device=DEV)
-            s["scales"] = torch.empty((c["rows"], c["n_in"] // 32), dtype=torch.uint8, device=DEV)
+            s["scales"] = torch.empty((c["rows"], B.mx_scale_bytes(c["n_in"])), dtype=torch.uint8, device=DEV)
             s["dims"] = B.make_mx_dims(c["rows"], c["N"], c["n_in"], c["n_out"], code[c["out"]])
             s["ws"] = B.alloc_bytes(B.mx_workspace_bytes(s["dims"]), DEV)
 
