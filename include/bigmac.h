@@ -117,7 +117,8 @@ typedef enum {
   BIGMAC_WS_LAYER_FORWARD = 3,   /* inference (saved == NULL)                                      */
   BIGMAC_WS_LAYER_TRAIN = 4,     /* forward with a saved block, and backward                       */
   BIGMAC_WS_SAVED = 5,           /* size of the saved-activation block of a training forward       */
-  BIGMAC_WS_AUX_LOSS = 6
+  BIGMAC_WS_AUX_LOSS = 6,
+  BIGMAC_WS_MX_GROUPED_FFN = 7
 } bigmac_ws_kind;
 
 /* Host only, touches no GPU.  Bytes of workspace the given call needs for these dims
@@ -352,6 +353,45 @@ size_t bigmac_norm_workspace_bytes(const bigmac_norm_dims *dims);
 int bigmac_norm_backward(const bigmac_norm_dims *dims, const bigmac_norm_params *params, const void *z, const void *y,
                          const void *du, const void *dz, void *dx, void *dy, void *d_gate, float *d_post_w,
                          float *d_post_b, float *d_pre_w, float *d_pre_b, void *ws, size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------ experts in 4 bits (serving) ---
+ * Microscaled 4-bit floating point: 32 values that follow each other along a product's contraction share a scale
+ * 2^E, E = max(floor(log2(largest magnitude)) - 2, -127), held as the byte E + 127; a value is held as the nearest of 0, 0.5, 1, 1.5, 2,
+ * 3, 4, 6 times the scale (codes 0 .. 7; ties to the even code, magnitudes past 6 as 6; bit 3: the sign).  A block with an
+ * infinity or NaN: byte 255, which stands for 32 NaN.  Products multiply the held values exactly and add in fp32. */
+
+/* Rows (operands of a product on the left): codes [rows, cols / 2], value 2i in the low half of byte i; scales [rows,
+ * bigmac_mx_scale_bytes(cols)]: 8 bytes per 256 columns, block b of them at byte (b % 2) * 4 + b / 2, unused bytes 0.  cols a multiple
+ * of 32.  Host only; 0 for a bad cols. */
+size_t bigmac_mx_scale_bytes(int64_t cols);
+int bigmac_mx_quantize(int64_t rows, int64_t cols, int32_t dtype, const void *src /*[rows,cols] dtype*/, void *codes, void *scales, void *stream);
+int bigmac_mx_dequantize(int64_t rows, int64_t cols, const void *codes, const void *scales, int32_t dtype, void *dst /*[rows,cols]*/, void *stream);
+
+/* Weights [groups, n_in, n_out] (blocks along n_in) laid out for the matrix instructions, codes and scales in one buffer of
+ * bigmac_mx_packed_bytes: done once, when the weights are loaded.  Unpacking gives the held values back.  n_in, n_out multiples
+ * of 64, up to 1024 groups (past it BIGMAC_ERR_TOO_LARGE).  bigmac_mx_packed_bytes: host only, 0 for bad sizes. */
+size_t bigmac_mx_packed_bytes(int32_t groups, int32_t n_in, int32_t n_out);
+int bigmac_mx_pack(int32_t groups, int32_t n_in, int32_t n_out, int32_t dtype, const void *w, void *packed, void *stream);
+int bigmac_mx_unpack(int32_t groups, int32_t n_in, int32_t n_out, const void *packed, int32_t dtype, void *w, void *stream);
+
+typedef struct {
+  int32_t rows, groups, n_in, n_out;
+  int32_t out_dtype;
+} bigmac_mx_dims;
+size_t bigmac_mx_workspace_bytes(const bigmac_mx_dims *dims); /* host only; 0 for bad dims */
+
+/* out[m, :] = A[m, :] W[e] (+ bias[e]) for the rows m of group e, offsets[e] <= m < offsets[e + 1] (device, [groups + 1], ascending from
+ * 0, up to rows; rows at or past offsets[groups] are left as they were).  offsets == NULL: one group of all rows (groups = 1; ws
+ * may be NULL).  A: codes and scales as bigmac_mx_quantize writes them; bias [groups, n_out] bf16 or NULL; out [rows, n_out]. */
+int bigmac_mx_product(const bigmac_mx_dims *dims, const void *codes, const void *scales, const int32_t *offsets, const void *packed,
+                      const void *bias, void *out, void *ws, size_t ws_bytes, void *stream);
+
+/* bigmac_grouped_ffn with the experts' matrices in 4 bits: the rows of x_perm are quantised, multiplied by w1, then bias, activation (fp32),
+ * the hidden rows quantised from fp32, multiplied by w2, bias, o_perm in bf16.  dtype BIGMAC_BF16 only (BIGMAC_ERR_UNSUPPORTED); w1 packed
+ * [N, win, hid], w2 packed [N, hid, win]; b1, b2 as there.  ws: BIGMAC_WS_MX_GROUPED_FFN.  Rows at or past expert_offsets[N] of o_perm
+ * are left as they were. */
+int bigmac_mx_grouped_ffn(const bigmac_dims *dims, const void *x_perm, const int32_t *expert_offsets, const void *w1, const void *w2,
+                          const void *b1, const void *b2, void *o_perm, void *ws, size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

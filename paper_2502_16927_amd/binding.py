@@ -13,7 +13,7 @@ import torch
 F32, BF16 = 0, 1
 ORDER_DCCA, ORDER_CDAC = 0, 1
 FLAG_ACCUMULATE, FLAG_OUT_BF16, FLAG_WIRE_BF16, FLAG_TILES_LARGE, FLAG_TILES_SMALL, FLAG_ROUTE_LOW, FLAG_NO_FUSED_DISPATCH = 1, 2, 4, 8, 16, 32, 64
-WS_ROUTE, WS_DISPATCH, WS_GROUPED_FFN, WS_LAYER_FORWARD, WS_LAYER_TRAIN, WS_SAVED, WS_AUX_LOSS = range(7)
+WS_ROUTE, WS_DISPATCH, WS_GROUPED_FFN, WS_LAYER_FORWARD, WS_LAYER_TRAIN, WS_SAVED, WS_AUX_LOSS, WS_MX_GROUPED_FFN = range(8)
 NORM_RMS, NORM_LAYER = 0, 1
 GATE_NONE, GATE_CHANNEL, GATE_TOKEN, GATE_FULL = range(4)
 NORM_POST, NORM_PRE, NORM_ACCUMULATE = 1, 2, 4
@@ -38,6 +38,10 @@ class NormDims(ctypes.Structure):
 
 class NormParams(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("post_w", "post_b", "pre_w", "pre_b", "gate")]
+
+
+class MxDims(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows", "groups", "n_in", "n_out", "out_dtype")]
 
 
 class BigmacError(RuntimeError):
@@ -101,6 +105,25 @@ def lib() -> ctypes.CDLL:
         L.bigmac_norm_forward.argtypes = [np_, pp, vp, vp, vp, vp, vp]
         L.bigmac_norm_backward.restype = ci
         L.bigmac_norm_backward.argtypes = [np_, pp] + [vp] * 12 + [sz, vp]
+        i32, i64, mp = ctypes.c_int32, ctypes.c_int64, ctypes.POINTER(MxDims)
+        L.bigmac_mx_scale_bytes.restype = sz
+        L.bigmac_mx_scale_bytes.argtypes = [i64]
+        L.bigmac_mx_packed_bytes.restype = sz
+        L.bigmac_mx_packed_bytes.argtypes = [i32] * 3
+        L.bigmac_mx_quantize.restype = ci
+        L.bigmac_mx_quantize.argtypes = [i64, i64, i32, vp, vp, vp, vp]
+        L.bigmac_mx_dequantize.restype = ci
+        L.bigmac_mx_dequantize.argtypes = [i64, i64, vp, vp, i32, vp, vp]
+        L.bigmac_mx_pack.restype = ci
+        L.bigmac_mx_pack.argtypes = [i32] * 4 + [vp] * 3
+        L.bigmac_mx_unpack.restype = ci
+        L.bigmac_mx_unpack.argtypes = [i32] * 3 + [vp, i32, vp, vp]
+        L.bigmac_mx_workspace_bytes.restype = sz
+        L.bigmac_mx_workspace_bytes.argtypes = [mp]
+        L.bigmac_mx_product.restype = ci
+        L.bigmac_mx_product.argtypes = [mp] + [vp] * 7 + [sz, vp]
+        L.bigmac_mx_grouped_ffn.restype = ci
+        L.bigmac_mx_grouped_ffn.argtypes = [dp] + [vp] * 8 + [sz, vp]
         L.bigmac_mfma_probe.restype = ci
         L.bigmac_mfma_probe.argtypes = [ci, ci, vp, ctypes.POINTER(ctypes.c_double), vp]
         _lib = L
@@ -110,7 +133,9 @@ def lib() -> ctypes.CDLL:
 EXPORTS = ("bigmac_workspace_bytes", "bigmac_status_string", "bigmac_forward_matrix_flops", "bigmac_permute_bytes",
            "bigmac_saved_layout", "bigmac_saved_aux_layout", "bigmac_aux_loss", "bigmac_route", "bigmac_dispatch", "bigmac_dispatch_static", "bigmac_grouped_ffn", "bigmac_combine",
            "bigmac_layer_forward", "bigmac_layer_backward", "bigmac_set_stage_events", "bigmac_stage_name", "bigmac_dispatch_folding", "bigmac_expert_pairing", "bigmac_topk_folding",
-           "bigmac_mfma_probe", "bigmac_gather_probe", "bigmac_norm_workspace_bytes", "bigmac_norm_forward", "bigmac_norm_backward")
+           "bigmac_mfma_probe", "bigmac_gather_probe", "bigmac_norm_workspace_bytes", "bigmac_norm_forward", "bigmac_norm_backward",
+           "bigmac_mx_scale_bytes", "bigmac_mx_quantize", "bigmac_mx_dequantize", "bigmac_mx_packed_bytes", "bigmac_mx_pack", "bigmac_mx_unpack",
+           "bigmac_mx_workspace_bytes", "bigmac_mx_product", "bigmac_mx_grouped_ffn")
 STAGE_COUNT = 22
 
 
@@ -257,6 +282,48 @@ def bigmac_norm_backward(dims, params, z, y, du, dz, dx, dy, d_gate, d_post_w, d
     _check(lib().bigmac_norm_backward(ctypes.byref(dims), ctypes.byref(params), _ptr(z), _ptr(y), _ptr(du), _ptr(dz), _ptr(dx), _ptr(dy), _ptr(d_gate),
                                       _ptr(d_post_w), _ptr(d_post_b), _ptr(d_pre_w), _ptr(d_pre_b), _ptr(ws), _nbytes(ws), _stream(stream)),
            "bigmac_norm_backward")
+
+
+def make_mx_dims(rows, groups, n_in, n_out, out_dtype=BF16) -> MxDims:
+    return MxDims(rows, groups, n_in, n_out, out_dtype)
+
+
+def mx_scale_bytes(cols: int) -> int:
+    return lib().bigmac_mx_scale_bytes(cols)
+
+
+def mx_packed_bytes(groups: int, n_in: int, n_out: int) -> int:
+    return lib().bigmac_mx_packed_bytes(groups, n_in, n_out)
+
+
+def mx_workspace_bytes(dims: MxDims) -> int:
+    return lib().bigmac_mx_workspace_bytes(ctypes.byref(dims))
+
+
+def bigmac_mx_quantize(rows, cols, dtype, src, codes, scales, stream=None):
+    _check(lib().bigmac_mx_quantize(rows, cols, dtype, _ptr(src), _ptr(codes), _ptr(scales), _stream(stream)), "bigmac_mx_quantize")
+
+
+def bigmac_mx_dequantize(rows, cols, codes, scales, dtype, dst, stream=None):
+    _check(lib().bigmac_mx_dequantize(rows, cols, _ptr(codes), _ptr(scales), dtype, _ptr(dst), _stream(stream)), "bigmac_mx_dequantize")
+
+
+def bigmac_mx_pack(groups, n_in, n_out, dtype, w, packed, stream=None):
+    _check(lib().bigmac_mx_pack(groups, n_in, n_out, dtype, _ptr(w), _ptr(packed), _stream(stream)), "bigmac_mx_pack")
+
+
+def bigmac_mx_unpack(groups, n_in, n_out, packed, dtype, w, stream=None):
+    _check(lib().bigmac_mx_unpack(groups, n_in, n_out, _ptr(packed), dtype, _ptr(w), _stream(stream)), "bigmac_mx_unpack")
+
+
+def bigmac_mx_product(dims, codes, scales, offsets, packed, bias, out, ws=None, stream=None):
+    _check(lib().bigmac_mx_product(ctypes.byref(dims), _ptr(codes), _ptr(scales), _ptr(offsets), _ptr(packed), _ptr(bias), _ptr(out), _ptr(ws), _nbytes(ws),
+                                   _stream(stream)), "bigmac_mx_product")
+
+
+def bigmac_mx_grouped_ffn(dims, x_perm, expert_offsets, w1, w2, o_perm, ws, b1=None, b2=None, stream=None):
+    _check(lib().bigmac_mx_grouped_ffn(ctypes.byref(dims), _ptr(x_perm), _ptr(expert_offsets), _ptr(w1), _ptr(w2), _ptr(b1), _ptr(b2), _ptr(o_perm), _ptr(ws),
+                                       _nbytes(ws), _stream(stream)), "bigmac_mx_grouped_ffn")
 
 
 def dispatch_folding(dims, training: bool) -> int:

@@ -311,6 +311,8 @@ size_t ragged_colsum_ws_bytes(int groups, int cols);
 int launch_ragged_colsum(int dtype, const void* src, long ld, int cols, const int32_t* offsets, int groups, float* out, int beta,
                          void* ws, hipStream_t s);
 
+size_t mx_ffn_ws_bytes(const bigmac_dims& D);   // workspace of bigmac_mx_grouped_ffn
+
 #define BIGMAC_CHECK_LAUNCH()                                   \
   do {                                                          \
     if (hipGetLastError() != hipSuccess) return BIGMAC_ERR_HIP; \

@@ -544,6 +544,7 @@ size_t bigmac_workspace_bytes(const bigmac_dims* D, int kind) {
     }
     case BIGMAC_WS_SAVED: return plan_saved(*D).total;
     case BIGMAC_WS_AUX_LOSS: return aux_loss_ws_bytes(*D);
+    case BIGMAC_WS_MX_GROUPED_FFN: return bf(*D) ? mx_ffn_ws_bytes(*D) : 0;
     default: return 0;
   }
 }

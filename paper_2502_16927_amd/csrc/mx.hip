@@ -1,0 +1,365 @@
+// Rows and weights into microscaled 4-bit floating point and back, and the C entry points of the 4-bit path.
+//
+// Conversions are bound by HBM: 2 or 4 bytes read, 17/32 of a byte written per value (back: the other way round).  Rows: eight
+// consecutive values a lane (16 bytes of bf16), a block's largest magnitude over four neighbouring lanes by register moves, the
+// comparison on the magnitudes' bits, which also finds infinities and NaN.  Weights: blocks run down the columns, so a lane takes
+// four columns x 32 inputs (reads of 512 or 1024 contiguous bytes a wavefront) and has whole blocks to itself.
+#include <algorithm>
+
+#include "mx.hpp"
+#include "tile_map.hpp"
+
+namespace bigmac {
+
+namespace {
+
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float* f);
+template <>
+__device__ __forceinline__ void load8<float>(const float* p, float* f) {
+  const float4 a = *(const float4*)p, b = *(const float4*)(p + 4);
+  f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
+  f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+}
+template <>
+__device__ __forceinline__ void load8<bf16_t>(const bf16_t* p, float* f) { unpack_bf16x8(*(const uint4*)p, f); }
+__device__ __forceinline__ void put8(float* p, const float* f) {
+  *(float4*)p = make_float4(f[0], f[1], f[2], f[3]);
+  *(float4*)(p + 4) = make_float4(f[4], f[5], f[6], f[7]);
+}
+__device__ __forceinline__ void put8(bf16_t* p, const float* f) { *(uint4*)p = pack_bf16x8(f); }
+
+constexpr int ROW_TURNS = 4;   // rows a thread takes
+
+// 1 << log_tx threads side by side on a row, the others on further rows
+template <typename T>
+__global__ __launch_bounds__(256) void mx_quantize_kernel(const T* __restrict__ src, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales, long rows,
+                                                          int cols, int log_tx, int scale_bytes) {
+  const int tx = threadIdx.x & ((1 << log_tx) - 1), ty = threadIdx.x >> log_tx, rows_at_once = 256 >> log_tx;
+  const int pieces = cols / 8;
+  for (int p = tx; p < scale_bytes * 4; p += 1 << log_tx) {   // (a multiple of 4 pieces; past the row's end only the unused scale bytes)
+#pragma unroll
+    for (int j = 0; j < ROW_TURNS; ++j) {
+      const long row = ((long)blockIdx.x * ROW_TURNS + j) * rows_at_once + ty;
+      if (row >= rows) break;
+      uint8_t* to = scales + row * scale_bytes + mx_scale_at((unsigned)p / 4);
+      if (p >= pieces) {
+        if ((p & 3) == 0) *to = 0;
+        continue;
+      }
+      float f[8];
+      load8(src + row * cols + (long)p * 8, f);
+      unsigned top = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(f[i]) & 0x7FFFFFFFu);
+      top = max(top, from_lane_xor<1>(top, 0));
+      top = max(top, from_lane_xor<2>(top, 0));
+      const unsigned byte = mx_scale_byte(top);
+      *(unsigned*)(codes + row * (cols / 2) + (long)p * 4) = mx_codes8(f, byte);
+      if ((p & 3) == 0) *to = (uint8_t)byte;
+    }
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void mx_dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, T* __restrict__ dst, long rows,
+                                                            int cols, int log_tx, int scale_bytes) {
+  const int tx = threadIdx.x & ((1 << log_tx) - 1), ty = threadIdx.x >> log_tx, rows_at_once = 256 >> log_tx;
+  const int pieces = cols / 8;
+  for (int p = tx; p < pieces; p += 1 << log_tx) {
+#pragma unroll
+    for (int j = 0; j < ROW_TURNS; ++j) {
+      const long row = ((long)blockIdx.x * ROW_TURNS + j) * rows_at_once + ty;
+      if (row >= rows) break;
+      float f[8];
+      mx_values8(*(const unsigned*)(codes + row * (cols / 2) + (long)p * 4), mx_scale(scales[row * scale_bytes + mx_scale_at((unsigned)p / 4)]), f);
+      put8(dst + row * cols + (long)p * 8, f);
+    }
+  }
+}
+
+// A thread's part of the weights: four output columns, one block out of each of up to four matrix instructions
+struct PackPlace {
+  long group;
+  int col, chunk, half;
+  bool any;
+};
+__device__ __forceinline__ PackPlace pack_place(long groups, int n_in, int n_out) {
+  const int quads = n_out / 4, chunks2 = (n_in + MX_CHUNK - 1) / MX_CHUNK * 2;
+  const long id = (long)blockIdx.x * 256 + threadIdx.x;
+  PackPlace t;
+  t.any = id < groups * chunks2 * quads;
+  t.col = (int)(id % quads) * 4;
+  const long rest = id / quads;
+  t.half = (int)(rest & 1);
+  t.chunk = (int)(rest % chunks2) >> 1;
+  t.group = rest / chunks2;
+  return t;
+}
+__device__ __forceinline__ void load4(const float* p, float* f) {
+  const float4 a = *(const float4*)p;
+  f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
+}
+__device__ __forceinline__ void load4(const bf16_t* p, float* f) {
+  const uint2 a = *(const uint2*)p;
+  f[0] = __uint_as_float(a.x << 16); f[1] = __uint_as_float(a.x & 0xFFFF0000u);
+  f[2] = __uint_as_float(a.y << 16); f[3] = __uint_as_float(a.y & 0xFFFF0000u);
+}
+__device__ __forceinline__ void put4(float* p, const float* f) { *(float4*)p = make_float4(f[0], f[1], f[2], f[3]); }
+__device__ __forceinline__ void put4(bf16_t* p, const float* f) { *(uint2*)p = make_uint2(f2bf_pair(f[0], f[1]), f2bf_pair(f[2], f[3])); }
+
+template <typename T>
+__global__ __launch_bounds__(256) void mx_pack_kernel(const T* __restrict__ w, uint8_t* __restrict__ packed, size_t scales_at, long groups, int n_in, int n_out) {
+  const PackPlace t = pack_place(groups, n_in, n_out);
+  if (!t.any) return;
+  const int steps = n_in / MX_STEP, chunks = (n_in + MX_CHUNK - 1) / MX_CHUNK, strips = n_out / 32;
+  const long strip = t.group * strips + t.col / 32;
+  const int lane = t.half * 32 + t.col % 32;
+  unsigned bytes[4] = {0, 0, 0, 0};
+#pragma unroll 1
+  for (int j = 0; j < 4; ++j) {
+    const int step = t.chunk * 4 + j;
+    if (step >= steps) break;
+    const T* from = w + (t.group * n_in + step * MX_STEP + t.half * MX_BLOCK) * n_out + t.col;
+    float f[4][32];
+#pragma unroll
+    for (int k = 0; k < 32; ++k) {
+      float v[4];
+      load4(from + (long)k * n_out, v);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) f[c][k] = v[c];
+    }
+    uint4* to = (uint4*)(packed + (strip * steps + step) * 1024) + lane;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      unsigned top = 0;
+#pragma unroll
+      for (int k = 0; k < 32; ++k) top = max(top, __float_as_uint(f[c][k]) & 0x7FFFFFFFu);
+      const unsigned byte = mx_scale_byte(top);
+      to[c] = make_uint4(mx_codes8(f[c], byte), mx_codes8(f[c] + 8, byte), mx_codes8(f[c] + 16, byte), mx_codes8(f[c] + 24, byte));
+      bytes[c] |= byte << (8 * j);
+    }
+  }
+  *(uint4*)(packed + scales_at + (strip * chunks + t.chunk) * 256 + lane * 4) = make_uint4(bytes[0], bytes[1], bytes[2], bytes[3]);
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void mx_unpack_kernel(const uint8_t* __restrict__ packed, size_t scales_at, T* __restrict__ w, long groups, int n_in, int n_out) {
+  const PackPlace t = pack_place(groups, n_in, n_out);
+  if (!t.any) return;
+  const int steps = n_in / MX_STEP, chunks = (n_in + MX_CHUNK - 1) / MX_CHUNK, strips = n_out / 32;
+  const long strip = t.group * strips + t.col / 32;
+  const int lane = t.half * 32 + t.col % 32;
+  const uint4 b = *(const uint4*)(packed + scales_at + (strip * chunks + t.chunk) * 256 + lane * 4);
+  const unsigned bytes[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll 1
+  for (int j = 0; j < 4; ++j) {
+    const int step = t.chunk * 4 + j;
+    if (step >= steps) break;
+    T* to = w + (t.group * n_in + step * MX_STEP + t.half * MX_BLOCK) * n_out + t.col;
+    const uint4* from = (const uint4*)(packed + (strip * steps + step) * 1024) + lane;
+    uint4 q[4];
+    float scale[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      q[c] = from[c];
+      scale[c] = mx_scale((bytes[c] >> (8 * j)) & 255u);
+    }
+#pragma unroll
+    for (int k8 = 0; k8 < 4; ++k8) {
+      float f[4][8];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) mx_values8(k8 == 0 ? q[c].x : k8 == 1 ? q[c].y : k8 == 2 ? q[c].z : q[c].w, scale[c], f[c]);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float v[4] = {f[0][k], f[1][k], f[2][k], f[3][k]};
+        put4(to + (long)(k8 * 8 + k) * n_out, v);
+      }
+    }
+  }
+}
+
+struct RowGrid {
+  unsigned blocks;
+  int log_tx;
+};
+RowGrid row_grid(long rows, long pieces) {
+  int log_tx = 2;
+  while (log_tx < 8 && (1l << log_tx) < pieces) ++log_tx;
+  const long per_block = (long)ROW_TURNS * (256 >> log_tx);
+  return {(unsigned)((rows + per_block - 1) / per_block), log_tx};
+}
+
+bool aligned(std::initializer_list<const void*> ps) {
+  for (const void* q : ps)
+    if ((size_t)q & 15) return false;
+  return true;
+}
+constexpr long MAX_ROWS = 0x7FFFFFFFl, MAX_COLS = 1l << 24;
+int check_rows(int64_t rows, int64_t cols, int dtype) {
+  if (rows < 1 || cols < 32 || cols % 32 || (dtype != BIGMAC_F32 && dtype != BIGMAC_BF16)) return BIGMAC_ERR_INVALID_ARG;
+  return rows > MAX_ROWS || cols > MAX_COLS ? BIGMAC_ERR_TOO_LARGE : BIGMAC_OK;
+}
+int check_weights(int32_t groups, int32_t n_in, int32_t n_out) {
+  if (groups < 1 || n_in < 64 || n_in % 64 || n_out < 64 || n_out % 64) return BIGMAC_ERR_INVALID_ARG;
+  return groups > 1024 || n_in > MAX_COLS || n_out > MAX_COLS ? BIGMAC_ERR_TOO_LARGE : BIGMAC_OK;
+}
+unsigned pack_blocks(long groups, long n_in, long n_out) {
+  return (unsigned)((groups * ((n_in + MX_CHUNK - 1) / MX_CHUNK) * 2 * (n_out / 4) + 255) / 256);
+}
+int check_mx(const bigmac_mx_dims* D) {
+  if (!D || D->rows < 1 || (D->out_dtype != BIGMAC_F32 && D->out_dtype != BIGMAC_BF16)) return BIGMAC_ERR_INVALID_ARG;
+  return check_weights(D->groups, D->n_in, D->n_out);
+}
+size_t mx_map_bytes(int rows, int groups) { return align_up(tile_map_ints(rows, groups, 32) * 4); }   // for every tile height
+
+struct FfnPlan {
+  size_t x_codes, x_scales, h_codes, h_scales, map, total;
+};
+FfnPlan plan_ffn(const bigmac_dims& D) {
+  const Widths W = widths(D);
+  const size_t rows = (size_t)D.T * D.k;
+  FfnPlan p;
+  p.x_codes = 0;
+  p.x_scales = align_up(rows * W.win / 2);
+  p.h_codes = p.x_scales + align_up(rows * mx_scale_bytes(W.win));
+  p.h_scales = p.h_codes + align_up(rows * W.hid / 2);
+  p.map = p.h_scales + align_up(rows * mx_scale_bytes(W.hid));
+  p.total = p.map + mx_map_bytes((int)rows, D.N);
+  return p;
+}
+
+}  // namespace
+
+int launch_mx_quantize(long rows, long cols, int dtype, const void* src, uint8_t* codes, uint8_t* scales, hipStream_t s) {
+  const int scale_bytes = (int)mx_scale_bytes(cols);
+  const RowGrid g = row_grid(rows, cols / 8);
+  if (dtype == BIGMAC_BF16) mx_quantize_kernel<bf16_t><<<g.blocks, 256, 0, s>>>((const bf16_t*)src, codes, scales, rows, (int)cols, g.log_tx, scale_bytes);
+  else mx_quantize_kernel<float><<<g.blocks, 256, 0, s>>>((const float*)src, codes, scales, rows, (int)cols, g.log_tx, scale_bytes);
+  BIGMAC_CHECK_LAUNCH();
+  return BIGMAC_OK;
+}
+
+size_t mx_ffn_ws_bytes(const bigmac_dims& D) { return plan_ffn(D).total; }
+
+}  // namespace bigmac
+
+using namespace bigmac;
+
+extern "C" {
+
+size_t bigmac_mx_scale_bytes(int64_t cols) { return cols < 1 || cols > MAX_COLS ? 0 : mx_scale_bytes(cols); }
+
+size_t bigmac_mx_packed_bytes(int32_t groups, int32_t n_in, int32_t n_out) {
+  return check_weights(groups, n_in, n_out) == BIGMAC_OK ? mx_packed(groups, n_in, n_out).bytes : 0;
+}
+
+int bigmac_mx_quantize(int64_t rows, int64_t cols, int32_t dtype, const void* src, void* codes, void* scales, void* stream) {
+  const int rc = check_rows(rows, cols, dtype);
+  if (rc) return rc;
+  if (!src || !codes || !scales || !aligned({src, codes, scales})) return BIGMAC_ERR_INVALID_ARG;
+  return launch_mx_quantize(rows, cols, dtype, src, (uint8_t*)codes, (uint8_t*)scales, (hipStream_t)stream);
+}
+
+int bigmac_mx_dequantize(int64_t rows, int64_t cols, const void* codes, const void* scales, int32_t dtype, void* dst, void* stream) {
+  const int rc = check_rows(rows, cols, dtype);
+  if (rc) return rc;
+  if (!dst || !codes || !scales || !aligned({dst, codes, scales})) return BIGMAC_ERR_INVALID_ARG;
+  const int scale_bytes = (int)mx_scale_bytes(cols);
+  const RowGrid g = row_grid(rows, cols / 8);
+  hipStream_t s = (hipStream_t)stream;
+  if (dtype == BIGMAC_BF16) mx_dequantize_kernel<bf16_t><<<g.blocks, 256, 0, s>>>((const uint8_t*)codes, (const uint8_t*)scales, (bf16_t*)dst, rows, (int)cols, g.log_tx, scale_bytes);
+  else mx_dequantize_kernel<float><<<g.blocks, 256, 0, s>>>((const uint8_t*)codes, (const uint8_t*)scales, (float*)dst, rows, (int)cols, g.log_tx, scale_bytes);
+  BIGMAC_CHECK_LAUNCH();
+  return BIGMAC_OK;
+}
+
+int bigmac_mx_pack(int32_t groups, int32_t n_in, int32_t n_out, int32_t dtype, const void* w, void* packed, void* stream) {
+  const int rc = check_weights(groups, n_in, n_out);
+  if (rc) return rc;
+  if ((dtype != BIGMAC_F32 && dtype != BIGMAC_BF16) || !w || !packed || !aligned({w, packed})) return BIGMAC_ERR_INVALID_ARG;
+  const size_t scales_at = mx_packed(groups, n_in, n_out).scales_at;
+  const unsigned blocks = pack_blocks(groups, n_in, n_out);
+  hipStream_t s = (hipStream_t)stream;
+  if (dtype == BIGMAC_BF16) mx_pack_kernel<bf16_t><<<blocks, 256, 0, s>>>((const bf16_t*)w, (uint8_t*)packed, scales_at, groups, n_in, n_out);
+  else mx_pack_kernel<float><<<blocks, 256, 0, s>>>((const float*)w, (uint8_t*)packed, scales_at, groups, n_in, n_out);
+  BIGMAC_CHECK_LAUNCH();
+  return BIGMAC_OK;
+}
+
+int bigmac_mx_unpack(int32_t groups, int32_t n_in, int32_t n_out, const void* packed, int32_t dtype, void* w, void* stream) {
+  const int rc = check_weights(groups, n_in, n_out);
+  if (rc) return rc;
+  if ((dtype != BIGMAC_F32 && dtype != BIGMAC_BF16) || !w || !packed || !aligned({w, packed})) return BIGMAC_ERR_INVALID_ARG;
+  const size_t scales_at = mx_packed(groups, n_in, n_out).scales_at;
+  const unsigned blocks = pack_blocks(groups, n_in, n_out);
+  hipStream_t s = (hipStream_t)stream;
+  if (dtype == BIGMAC_BF16) mx_unpack_kernel<bf16_t><<<blocks, 256, 0, s>>>((const uint8_t*)packed, scales_at, (bf16_t*)w, groups, n_in, n_out);
+  else mx_unpack_kernel<float><<<blocks, 256, 0, s>>>((const uint8_t*)packed, scales_at, (float*)w, groups, n_in, n_out);
+  BIGMAC_CHECK_LAUNCH();
+  return BIGMAC_OK;
+}
+
+size_t bigmac_mx_workspace_bytes(const bigmac_mx_dims* D) { return check_mx(D) == BIGMAC_OK ? mx_map_bytes(D->rows, D->groups) : 0; }
+
+int bigmac_mx_product(const bigmac_mx_dims* D, const void* codes, const void* scales, const int32_t* offsets, const void* packed, const void* bias, void* out,
+                      void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_mx(D);
+  if (rc) return rc;
+  if (!codes || !scales || !packed || !out || !aligned({codes, scales, packed, bias, out})) return BIGMAC_ERR_INVALID_ARG;
+  if (!offsets && D->groups != 1) return BIGMAC_ERR_INVALID_ARG;
+  hipStream_t s = (hipStream_t)stream;
+  MxProduct p{};
+  p.codes = (const uint8_t*)codes; p.scales = (const uint8_t*)scales; p.packed = (const uint8_t*)packed; p.bias = (const bf16_t*)bias;
+  p.out = out;
+  p.rows = D->rows; p.groups = D->groups; p.n_in = D->n_in; p.n_out = D->n_out;
+  p.epilogue = D->out_dtype == BIGMAC_F32 ? MX_STORE_F32 : MX_STORE_BF16;
+  if (offsets) {
+    if (!ws || !aligned({ws})) return BIGMAC_ERR_INVALID_ARG;
+    if (ws_bytes < mx_map_bytes(D->rows, D->groups)) return BIGMAC_ERR_WORKSPACE;
+    p.offsets = offsets;
+    p.tile_map = (const int*)ws;
+    TileMapJobs maps{};
+    maps.tile_rows[0] = mx_tile_rows(D->rows, D->groups);
+    maps.map[0] = (int*)ws;
+    rc = launch_build_tile_map(offsets, D->groups, maps, s);
+    if (rc) return rc;
+  }
+  return launch_mx_product(p, s);
+}
+
+int bigmac_mx_grouped_ffn(const bigmac_dims* D, const void* x_perm, const int32_t* expert_offsets, const void* w1, const void* w2, const void* b1, const void* b2,
+                          void* o_perm, void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_dims(D);
+  if (rc) return rc;
+  if (D->dtype != BIGMAC_BF16) return BIGMAC_ERR_UNSUPPORTED;
+  const Widths W = widths(*D);
+  rc = check_weights(D->N, W.win, W.hid);
+  if (rc) return rc;
+  if (!x_perm || !expert_offsets || !w1 || !w2 || !o_perm || !ws || !aligned({x_perm, w1, w2, b1, b2, o_perm, ws})) return BIGMAC_ERR_INVALID_ARG;
+  const FfnPlan plan = plan_ffn(*D);
+  if (ws_bytes < plan.total) return BIGMAC_ERR_WORKSPACE;
+  hipStream_t s = (hipStream_t)stream;
+  const int rows = (int)((long)D->T * D->k);
+  uint8_t* base = (uint8_t*)ws;
+  TileMapJobs maps{};
+  maps.tile_rows[0] = mx_tile_rows(rows, D->N);
+  maps.map[0] = (int*)(base + plan.map);
+  rc = launch_build_tile_map(expert_offsets, D->N, maps, s);
+  if (rc) return rc;
+  rc = launch_mx_quantize(rows, W.win, BIGMAC_BF16, x_perm, base + plan.x_codes, base + plan.x_scales, s);
+  if (rc) return rc;
+  MxProduct p{};
+  p.codes = base + plan.x_codes; p.scales = base + plan.x_scales; p.packed = (const uint8_t*)w1; p.bias = (const bf16_t*)b1;
+  p.offsets = expert_offsets; p.tile_map = maps.map[0];
+  p.out = base + plan.h_codes; p.out_scales = base + plan.h_scales;
+  p.rows = rows; p.groups = D->N; p.n_in = W.win; p.n_out = W.hid; p.epilogue = MX_GELU_CODES;
+  rc = launch_mx_product(p, s);
+  if (rc) return rc;
+  p.codes = base + plan.h_codes; p.scales = base + plan.h_scales; p.packed = (const uint8_t*)w2; p.bias = (const bf16_t*)b2;
+  p.out = o_perm; p.out_scales = nullptr;
+  p.n_in = W.hid; p.n_out = W.win; p.epilogue = MX_STORE_BF16;
+  return launch_mx_product(p, s);
+}
+
+}  // extern "C"

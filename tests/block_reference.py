@@ -66,7 +66,7 @@ HELD = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
 def quantise(v):
     """(codes [.., n] 0..15, scale bytes [.., n / 32], values [.., n]) of rows in blocks of 32.  A block with an infinity or NaN: byte 255, codes 0, NaN."""
     v = np.asarray(v, np.float64)
-    b = v.reshape(*v.shape[:-1], -1, 32)
+    b = v.reshape(*v.shape[:-1], v.shape[-1] // 32, 32)
     top = np.abs(b).max(-1)
     finite = np.isfinite(top)
     power = np.frexp(np.where(finite, top, 1.0))[1] - 1                       # floor(log2 top)

@@ -1,0 +1,296 @@
+"""The 4-bit path against plain 64-bit arithmetic (block_reference): conversions exactly, products within the rounding of fp32 sums.
+
+Tolerances.  u = 2^-24.  The held values' products are exact.  A matrix instruction adds 64 of them, in whatever order at most 64 additions
+for a term, and n / 64 instructions follow each other: 64 + n / 64 additions, each off by at most a step of the partial sum (2 u of it;
+the matrix cores may cut instead of rounding), and one more for the bias.  The FFN's hidden rows are
+rounded to 4 bits from fp32: where a hidden value lies within its own error of a border, it may fall on either side, and the output may
+be off by that step times the weight."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2502_16927_amd import binding as B
+import block_reference as R
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPE = {"f32": torch.float32, "bf16": torch.bfloat16}
+CODE = {"f32": B.F32, "bf16": B.BF16}
+
+
+def up(t):
+    return t.double().cpu().numpy()
+
+
+def scale_place(blocks):
+    b = np.arange(blocks)
+    return (b // 8) * 8 + (b % 2) * 4 + (b % 8) // 2
+
+
+def quantised(src):
+    """Codes and scales of the library, as numpy: codes [rows, cols], scale bytes in block order, and the buffers."""
+    rows, cols = src.shape
+    codes = torch.full((rows, cols // 2), 0xEE, dtype=torch.uint8, device=DEV)
+    scales = torch.full((rows, B.mx_scale_bytes(cols)), 0xEE, dtype=torch.uint8, device=DEV)
+    B.bigmac_mx_quantize(rows, cols, B.BF16 if src.dtype == torch.bfloat16 else B.F32, src, codes, scales)
+    c, s = codes.cpu().numpy().astype(np.int64), scales.cpu().numpy().astype(np.int64)
+    used = scale_place(cols // 32)
+    assert (np.delete(s, used, 1) == 0).all(), "unused scale bytes"
+    return np.stack([c & 15, c >> 4], 2).reshape(rows, cols), s[:, used], codes, scales
+
+
+def check_rows(src):
+    rows, cols = src.shape
+    want_codes, want_scales, want = R.quantise(up(src))
+    got_codes, got_scales, codes, scales = quantised(src)
+    assert np.array_equal(got_scales, want_scales)
+    assert np.array_equal(got_codes, want_codes)
+    for t in ("f32", "bf16"):
+        back = torch.full((rows, cols), 7.0, dtype=TYPE[t], device=DEV)
+        B.bigmac_mx_dequantize(rows, cols, codes, scales, CODE[t], back)
+        assert np.array_equal(up(back), want, equal_nan=True)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(1, 32), (1, 64), (3, 96), (65, 288), (130, 1024), (7, 4096), (513, 320), (2, 8224)])
+def test_rows_to_four_bits_and_back(rows, cols, dtype):
+    g = torch.Generator(device=DEV).manual_seed(rows + cols)
+    src = torch.randn((rows, cols), generator=g, device=DEV) * torch.exp2(torch.randint(-30, 30, (rows, 1), generator=g, device=DEV).float())
+    check_rows(src.to(TYPE[dtype]))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_borders_ties_zeros_and_extremes(dtype):
+    """Every middle between two held values, its neighbours, largest magnitudes at and next to powers of two, zeros of both signs, the
+    smallest and the largest numbers of the type, blocks with an infinity or NaN beside whole ones."""
+    t = TYPE[dtype]
+    grid = np.array([0, 0.25, 0.5, 0.75, 1, 1.25, 1.5, 1.75, 2, 2.5, 3, 3.5, 4, 5, 6, 7])
+    rows = []
+    for power in (-140, -133, -128, -126, -125, -100, -3, 0, 1, 90, 120):
+        for top in (4.0, 6.0, 7.5, 1.0, 2.0):
+            base = torch.tensor(np.concatenate([grid[grid <= top], [top]]) * 2.0 ** power, dtype=torch.float64).to(t)
+            near = torch.cat([base, torch.nextafter(base.float(), torch.tensor(float("inf"))).to(t), -base])
+            block = torch.zeros(96, dtype=t)
+            block[:min(96, near.numel())] = near[:96]
+            block[block.abs() > abs(float(base[-1]))] = base[-1]
+            rows.append(block)
+    rows.append(torch.zeros(96, dtype=t))
+    rows.append(-torch.zeros(96, dtype=t))
+    rows.append(torch.full((96,), torch.finfo(t).max, dtype=t))
+    rows.append(torch.full((96,), torch.finfo(t).tiny, dtype=t))
+    for bad in (float("inf"), float("-inf"), float("nan")):
+        r = torch.linspace(-5, 5, 96).to(t)
+        r[40] = bad
+        rows.append(r)
+    check_rows(torch.stack(rows).to(DEV))
+
+
+def pack(w):
+    groups, n_in, n_out = w.shape
+    packed = torch.full((B.mx_packed_bytes(groups, n_in, n_out),), 0xEE, dtype=torch.uint8, device=DEV)
+    B.bigmac_mx_pack(groups, n_in, n_out, B.BF16 if w.dtype == torch.bfloat16 else B.F32, w, packed)
+    return packed
+
+
+def held(w):
+    """Held values of weights [groups, n_in, n_out]: blocks along n_in."""
+    return np.swapaxes(R.quantise(np.swapaxes(up(w), 1, 2).copy())[2], 1, 2)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("groups,n_in,n_out", [(1, 64, 64), (3, 192, 64), (2, 320, 192), (5, 1024, 128)])
+def test_weights_packed_and_unpacked(groups, n_in, n_out, dtype):
+    g = torch.Generator(device=DEV).manual_seed(n_in)
+    w = (torch.randn((groups, n_in, n_out), generator=g, device=DEV) * 0.02).to(TYPE[dtype])
+    w[0, :32, 5] = 0.0
+    w[groups - 1, n_in - 3, n_out - 1] = float("inf")
+    packed = pack(w)
+    for t in ("f32", "bf16"):
+        back = torch.empty((groups, n_in, n_out), dtype=TYPE[t], device=DEV)
+        B.bigmac_mx_unpack(groups, n_in, n_out, packed, CODE[t], back)
+        assert np.array_equal(up(back), held(w), equal_nan=True)
+    again = pack(torch.nan_to_num(back, nan=float("inf")))
+    assert torch.equal(again, packed)                                # held values are held as themselves
+
+
+def offsets_of(counts):
+    return torch.tensor(np.concatenate([[0], np.cumsum(counts)]), dtype=torch.int32, device=DEV)
+
+
+def product(x, counts, w, bias=None, out="f32", spare=0):
+    """bigmac_mx_product on quantised rows; counts None: dense.  spare: rows of the buffers behind the last group."""
+    groups, n_in, n_out = w.shape
+    rows = x.shape[0]
+    _, _, codes, scales = quantised(x)
+    dims = B.make_mx_dims(rows, groups, n_in, n_out, CODE[out])
+    ws = torch.full((max(B.mx_workspace_bytes(dims), 256),), 0xEE, dtype=torch.uint8, device=DEV)
+    got = torch.full((rows, n_out), 7.0, dtype=TYPE[out], device=DEV)
+    B.bigmac_mx_product(dims, codes, scales, None if counts is None else offsets_of(counts), pack(w), bias, got, ws)
+    return got
+
+
+def check_product(counts, n_in, n_out, out="f32", bias=False, spare=0, dense=False, seed=0):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    groups, rows = len(counts), int(sum(counts)) + spare
+    x = torch.randn((rows, n_in), generator=g, device=DEV).to(torch.bfloat16)
+    w = (torch.randn((groups, n_in, n_out), generator=g, device=DEV) * torch.exp2(torch.randint(-4, 5, (groups, n_in, 1), generator=g, device=DEV).float())).to(torch.bfloat16)
+    b = torch.randn((groups, n_out), generator=g, device=DEV).to(torch.bfloat16) if bias else None
+    got = up(product(x, None if dense else counts, w, b, out))
+    xq, wq = R.quantise(up(x))[2], held(w)
+    at = 0
+    for e, n in enumerate(counts):
+        a = xq[at:at + n]
+        want, size = a @ wq[e], np.abs(a) @ np.abs(wq[e])
+        if bias:
+            want, size = want + up(b)[e], size + np.abs(up(b)[e])
+        limit = 2 * (65 + n_in / 64) * R.U32 * size + R.HALF_STEP[out] * np.abs(want) * (1 + 2.0 ** -10)
+        off = np.abs(got[at:at + n] - want)
+        assert (off <= limit).all(), f"group {e} of {n} rows: {int((off > limit).sum())} of {off.size} off, worst {np.nanmax(off / limit)} of the limit"
+        at += n
+    assert (got[at:] == 7.0).all(), "rows behind the last group"
+
+
+# row counts around the tiles' edges, groups without rows at the start, in between and at the end, inputs that end inside a chunk
+@pytest.mark.parametrize("n_in,n_out", [(64, 64), (192, 320), (256, 64), (320, 128), (1024, 192), (4096, 64)])
+@pytest.mark.parametrize("counts", [[1], [0, 1, 0], [31, 32, 33, 0], [5, 0, 63, 64, 65, 1], [127, 128, 129], [300, 0, 1, 270]], ids=str)
+def test_ragged_products(counts, n_in, n_out):
+    print(f"products of {counts} rows, {n_in} -> {n_out}", flush=True)
+    check_product(counts, n_in, n_out, seed=n_in)
+    check_product(counts, n_in, n_out, out="bf16", bias=True, spare=37, seed=n_in + 1)
+
+
+@pytest.mark.parametrize("rows", [1, 2, 33, 64, 100, 129, 1000])
+def test_dense_products(rows):
+    check_product([rows], 576, 448, dense=True, bias=rows % 2 == 0, out="bf16" if rows > 64 else "f32")
+
+
+def test_many_groups():
+    rng = np.random.default_rng(3)
+    check_product(list(rng.integers(0, 5, 700)), 64, 64)
+
+
+def test_large_ragged_product_against_an_exact_one():
+    """Thousands of rows over uneven groups: the values are small integers, every product and sum is exact."""
+    g = torch.Generator(device=DEV).manual_seed(4)
+    counts = [1500, 0, 3, 700, 2049, 31]
+    held_ints = torch.tensor([0.0, 1.0, 2.0, 3.0, 4.0, 6.0], device=DEV)
+    pick = lambda *shape: held_ints[torch.randint(0, 6, shape, generator=g, device=DEV)] * (torch.randint(0, 2, shape, generator=g, device=DEV) * 2 - 1)  # noqa: E731
+    rows, n_in, n_out = sum(counts), 1088, 640
+    x, w = pick(rows, n_in), pick(len(counts), n_in, n_out)
+    x[:, ::32], w[:, ::32] = 6.0, 4.0                                # every block's scale is 1
+    got = product(x.to(torch.bfloat16), counts, w.to(torch.bfloat16), out="f32")
+    at = 0
+    for e, n in enumerate(counts):
+        assert torch.equal(got[at:at + n], (x[at:at + n].double() @ w[e].double()).float()), e
+        at += n
+
+
+def test_a_row_that_is_not_finite_stays_alone():
+    g = torch.Generator(device=DEV).manual_seed(8)
+    x = torch.randn((70, 256), generator=g, device=DEV).to(torch.bfloat16)
+    w = torch.randn((2, 256, 128), generator=g, device=DEV).to(torch.bfloat16)
+    want = product(x, [40, 30], w)
+    x[5, 100], x[60, 0] = float("nan"), float("inf")
+    got = product(x, [40, 30], w)
+    keep = [r for r in range(70) if r not in (5, 60)]
+    assert torch.equal(got[keep], want[keep]) and torch.isnan(got[5]).all() and torch.isnan(got[60]).all()
+
+
+# ------------------------------------------------------------------ the experts' FFN
+
+def ffn_reference(x, counts, w1, w2, b1, b2):
+    """(output, tolerance) per row: see the head of this file."""
+    outs, limits, at = [], [], 0
+    xq = R.quantise(x)[2]
+    for e, n in enumerate(counts):
+        a = xq[at:at + n]
+        pre, size = a @ w1[e], np.abs(a) @ np.abs(w1[e])
+        if b1 is not None:
+            pre, size = pre + b1[e], size + np.abs(b1[e])
+        h = R.gelu(pre)
+        # |gelu'| < 1.13; the library's GELU is within 4e-7 of gelu
+        off = 1.13 * 2 * (65 + a.shape[1] / 64) * R.U32 * size + 4e-7 + 4 * R.U32 * np.abs(h)
+        q = R.quantise(h)[2]
+        moved = np.zeros_like(q)
+        for direction in (1.0, -1.0):                                # all magnitudes a little larger, a little smaller: also across a scale's border
+            there = R.quantise(np.where(h < 0, -1.0, 1.0) * np.maximum(np.abs(h) + direction * off, 0.0))[2]
+            moved = np.maximum(moved, np.abs(there - q))
+        want, osize = q @ w2[e], np.abs(q) @ np.abs(w2[e])
+        if b2 is not None:
+            want, osize = want + b2[e], osize + np.abs(b2[e])
+        outs.append(want)
+        limits.append(2 * (65 + h.shape[1] / 64) * R.U32 * osize + R.HALF_STEP["bf16"] * np.abs(want) * (1 + 2.0 ** -10) + (1 + R.HALF_STEP["bf16"]) * (moved @ np.abs(w2[e])))
+        at += n
+    return np.concatenate(outs), np.concatenate(limits)
+
+
+class Ffn:
+    def __init__(self, T, k, N, r, h, counts, bias, order=B.ORDER_DCCA, seed=0):
+        g = torch.Generator(device=DEV).manual_seed(seed)
+        self.counts, rows = counts, T * k
+        self.dims = B.make_dims(T, r if order == B.ORDER_CDAC else 4 * r, h if order == B.ORDER_CDAC else r, N, k, h, order=order)
+        rand = lambda std, *shape: (torch.randn(shape, generator=g, device=DEV) * std).to(torch.bfloat16)  # noqa: E731
+        self.x, w1, w2 = rand(1.0, rows, r), rand(2.0 / r ** 0.5, N, r, h), rand(0.02, N, h, r)
+        self.b1, self.b2 = (rand(0.3, N, h), rand(0.02, N, r)) if bias else (None, None)
+        self.w1, self.w2, self.h1, self.h2 = pack(w1), pack(w2), held(w1), held(w2)
+        self.offsets = offsets_of(counts)
+        self.out = torch.full((rows, r), 7.0, dtype=torch.bfloat16, device=DEV)
+        self.ws = torch.full((B.workspace_bytes(self.dims, B.WS_MX_GROUPED_FFN),), 0xEE, dtype=torch.uint8, device=DEV)
+
+    def run(self, stream=None):
+        B.bigmac_mx_grouped_ffn(self.dims, self.x, self.offsets, self.w1, self.w2, self.out, self.ws, b1=self.b1, b2=self.b2, stream=stream)
+
+    def check(self):
+        rows = sum(self.counts)
+        want, limit = ffn_reference(up(self.x)[:rows], self.counts, self.h1, self.h2, None if self.b1 is None else up(self.b1), None if self.b2 is None else up(self.b2))
+        off = np.abs(up(self.out)[:rows] - want)
+        assert (off <= limit).all(), f"{int((off > limit).sum())} of {off.size} off, worst {np.nanmax(off / limit)} of the limit"
+        assert (self.out[rows:] == 7.0).all(), "rows behind the last expert"
+        # the tolerance for hidden values next to a border is an exception, not the rule
+        assert np.mean(limit > 0.05 * np.sqrt(np.mean(want ** 2))) < 0.2
+
+
+@pytest.mark.parametrize("T,k,N,r,h,counts", [
+    (1, 1, 1, 64, 64, [1]),
+    (1, 2, 4, 128, 256, [0, 1, 1, 0]),
+    (32, 8, 8, 192, 448, [40, 0, 31, 33, 64, 1, 86, 1]),
+    (40, 4, 4, 320, 640, [70, 64, 20, 6]),
+    (200, 2, 3, 256, 576, [129, 0, 271]),
+    (64, 2, 2, 1024, 128, [128, 0]),
+], ids=str)
+@pytest.mark.parametrize("bias", [False, True])
+def test_experts(T, k, N, r, h, counts, bias):
+    print(f"experts T {T} k {k} N {N} r {r} h {h} {counts}", flush=True)
+    f = Ffn(T, k, N, r, h, counts, bias, seed=r)
+    f.run()
+    f.check()
+
+
+def test_experts_of_the_fine_grained_order_and_dropped_pairs():
+    """win = d, hid = r; fewer rows than T k (a capacity dropped some): the rest of o_perm stays as it was."""
+    f = Ffn(50, 2, 4, 256, 192, [20, 3, 0, 41], True, order=B.ORDER_CDAC)
+    f.run()
+    f.check()
+
+
+def test_experts_on_another_stream_and_in_a_graph():
+    f = Ffn(60, 4, 6, 256, 512, [100, 0, 33, 64, 42, 1], True)
+    f.run()
+    f.check()
+    want = f.out.clone()
+    s = torch.cuda.Stream()
+    f.out.fill_(7.0)
+    torch.cuda.synchronize()
+    f.run(stream=s.cuda_stream)
+    s.synchronize()
+    assert torch.equal(f.out, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        f.run()
+    for replay in range(4):
+        f.out.fill_(7.0)
+        f.ws.fill_(0xEE)
+        _ = (f.x.float() * 2).sum().item()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(f.out, want), replay
