@@ -7,146 +7,298 @@
 #include <type_traits>
 
 #include "mx.hpp"
-#include "tile_map.hpp"
+#include "gemm_core.hpp"
 
 namespace bigmac {
 
 namespace {
 
 typedef int i32x8_t __attribute__((ext_vector_type(8)));
-typedef float f32x16_t __attribute__((ext_vector_type(16)));
-typedef const int __attribute__((address_space(4))) * table_ptr_t;
-__device__ __forceinline__ int table_at(const int* table, int i) { return ((table_ptr_t)(unsigned long long)table)[i]; }
-
-typedef unsigned int q4_t __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t scalar_buffer(size_t at, size_t bytes) {
   const unsigned lo = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)at), hi = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(at >> 32));
   return __builtin_amdgcn_make_buffer_rsrc((void*)(((size_t)hi << 32) | lo), 0, __builtin_amdgcn_readfirstlane((int)bytes), 0x00020000);
 }
 template <int J>
-__device__ __forceinline__ f32x16_t mx_mfma(const q4_t& w, unsigned ws, const q4_t& a, unsigned as, f32x16_t c) {
+__device__ __forceinline__ f32x16_t mx_mfma(const u32x4_t& w, unsigned ws, const u32x4_t& a, unsigned as, f32x16_t c) {
   const i32x8_t W = {(int)w.x, (int)w.y, (int)w.z, (int)w.w, 0, 0, 0, 0}, A = {(int)a.x, (int)a.y, (int)a.z, (int)a.w, 0, 0, 0, 0};
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(W, A, c, 4, 4, J, (int)ws, J, (int)as);   // 4: e2m1
 }
+// a value that an LDS read written in assembly delivers: usable behind the wait in front of this call
+template <typename T>
+__device__ __forceinline__ void hold(T& v) { asm volatile("" : "+v"(v)); }
+template <int OFFSET>
+__device__ __forceinline__ void lds_read_b32(unsigned addr, unsigned& v) { asm volatile("ds_read_b32 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(OFFSET) : "memory"); }
 
-// 16-byte piece index in the LDS of piece c (of 8) of a row of 256 4-bit values: 16 consecutive rows at one piece lie on 16 different
-// groups of 4 banks
-__device__ __forceinline__ int piece_at(int row, int c) { return row * 8 + (c ^ ((row >> 1) & 7)); }
+// GELU for 4-bit results: a polynomial of degree 6 for log2 of the normal tail (weighted least squares of |a| tail(|a|): absolute error
+// of the GELU under 8e-8, relative error of the tail under 5e-6 up to |a| = 2 and 4e-4 at 4; a step of a 4-bit value is an eighth of it and more).
+// |a| is cut off at 9, where the tail's fit is 2^-62.  fmed3 with infinity: max(a, 0) in one instruction.
+__device__ __forceinline__ float gelu_mx_f(float a) {
+  const float x = __builtin_amdgcn_fmed3f(fabsf(a), 0.0f, 9.0f);
+  float q = fmaf(x, 3.31598240e-05f, -7.69719801e-04f);
+  q = fmaf(x, q, 8.08210559e-03f);
+  q = fmaf(x, q, -5.34138962e-02f);
+  q = fmaf(x, q, -4.58769884e-01f);
+  q = fmaf(x, q, -1.15120198e+00f);
+  q = fmaf(x, q, -9.99993041e-01f);
+  return fmaf(-fabsf(a), __builtin_amdgcn_exp2f(q), __builtin_amdgcn_fmed3f(a, 0.0f, INFINITY));
+}
+// largest magnitude of 16 values, NaN if one is
+__device__ __forceinline__ float top_of(const float (&f)[16]) {
+  float t = f[0];
+#pragma unroll
+  for (int v = 0; v < 16; v += 2) asm("v_maximum3_f32 %0, |%1|, |%2|, |%0|" : "+v"(t) : "v"(f[v]), "v"(f[v + 1]));
+  return t;
+}
+// eight values over 2^(byte - 127), byte 1 .. 254: the conversion divides by its scale operand
+__device__ __forceinline__ unsigned mx_codes8_scaled(const float* f, unsigned byte) {
+  const float scale = __uint_as_float(byte << 23);
+  unsigned r = 0;
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, f[0], f[1], scale, 0);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, f[2], f[3], scale, 1);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, f[4], f[5], scale, 2);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, f[6], f[7], scale, 3);
+  return byte == 255u ? 0u : r;
+}
 
-// MT x 32 rows, 4 wavefronts side by side with NS x 32 columns each
-template <int MT, int NS, int EPI>
-__global__ __launch_bounds__(256, 2) void mx_product_kernel(MxProduct p) {
-  constexpr int BM = MT * 32, STRIPS = 4 * NS;
-  constexpr int PIECES = BM * 8 / 256;   // of A per thread and chunk
-  __shared__ uint4 a_codes[2][BM * 8];
-  __shared__ unsigned a_scales[2][BM * 2];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+// Which tile a workgroup has, and what it needs of it
+struct MxTile {
+  int group, m0, m_rows, strip0;   // strip0: first 32 columns of the workgroup
+  bool valid;
+};
+template <int BM, int STRIPS>
+__device__ __forceinline__ MxTile mx_tile(const MxProduct& p) {
+  MxTile t;
   const int strips = p.n_out / 32, gx = (strips + STRIPS - 1) / STRIPS;
   const int tiles = p.offsets ? table_at(p.tile_map, 0) : (p.rows + BM - 1) / BM;
   // consecutive workgroups go to the 8 XCDs in turn: each XCD gets a run of consecutive tiles, column tiles fastest
   const long total = (long)tiles * gx;
   const long per_xcd = (total + 7) / 8, slot = blockIdx.x >> 3;
   const long id = (long)(blockIdx.x & 7) * per_xcd + slot;
-  if (slot >= per_xcd || id >= total) return;
-  const int tile = (int)(id / gx), strip0 = (int)(id % gx) * STRIPS + wave * NS;
-  int group = 0, m0 = tile * BM, m_end = p.rows;
+  t.valid = slot < per_xcd && id < total;
+  if (!t.valid) return t;
+  const int tile = (int)(id / gx);
+  t.strip0 = (int)(id % gx) * STRIPS;
+  int m_end = p.rows;
+  t.group = 0;
+  t.m0 = tile * BM;
   if (p.offsets) {
-    group = table_at(p.tile_map, TILE_MAP_HEADER + p.groups + 2 * tile);
-    m0 = table_at(p.tile_map, TILE_MAP_HEADER + p.groups + 1 + 2 * tile);
-    m_end = table_at(p.offsets, group + 1);
+    t.group = table_at(p.tile_map, TILE_MAP_HEADER + p.groups + 2 * tile);
+    t.m0 = table_at(p.tile_map, TILE_MAP_HEADER + p.groups + 1 + 2 * tile);
+    m_end = table_at(p.offsets, t.group + 1);
   }
-  const int m_rows = min(m_end - m0, BM);
+  t.m_rows = min(m_end - t.m0, BM);
+  return t;
+}
+
+// Results of a sub-tile of 32 rows x 32 columns.  Lane l: row l % 32, columns 8 q + 4 (l / 32) + 0 .. 3 in values 4 q .. 4 q + 3.
+template <int EPI>
+__device__ __forceinline__ void mx_store(const MxProduct& p, const f32x16_t& acc, const float (&bias)[16], bool biased, int row, bool live, int col0, int lane) {
+  const int half = lane >> 5;
+  const size_t at = (size_t)row;
+  float f[16];
+#pragma unroll
+  for (int v = 0; v < 16; ++v) f[v] = acc[v];
+  if (biased)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) f[v] += bias[v];
+  if (EPI == MX_GELU_CODES) {
+#pragma unroll
+    for (int v = 0; v < 16; ++v) f[v] = gelu_mx_f(f[v]);
+    unsigned top = __float_as_uint(top_of(f));
+    top = max(top, from_lane_xor<32>(top, lane));   // (magnitudes and NaN are ordered as integers; the NaN may have its sign set: the shift below drops it)
+    top &= 0x7FFFFFFFu;
+    // the smallest scale here is 2^-126: values of a block under 2^-124 that 2^-127 would hold better
+    const unsigned byte = max(mx_scale_byte(top), 1u);
+    const unsigned lo = mx_codes8_scaled(f, byte), hi = mx_codes8_scaled(f + 8, byte);   // halfword q: this lane's four columns of quad q
+    // the lower lane puts columns 0 .. 15 together, the upper one 16 .. 31: one exchange
+    const unsigned got = from_lane_xor<32>(half ? lo : hi, lane);
+    const unsigned mine = half ? hi : lo;
+    const unsigned even = half ? got : mine, odd = half ? mine : got;      // quads of the lower lane, of the upper lane
+    if (live) {
+      *(uint2*)((uint8_t*)p.out + at * (p.n_out / 2) + col0 / 2 + 8 * half) =
+          make_uint2((even & 0xFFFFu) | (odd << 16), (even >> 16) | (odd & 0xFFFF0000u));
+      if (!half) p.out_scales[at * ((p.n_out + MX_CHUNK - 1) / MX_CHUNK * 8) + mx_scale_at((unsigned)col0 / 32)] = (uint8_t)byte;
+    }
+  } else if (EPI == MX_STORE_F32) {
+    if (live)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) *(float4*)((float*)p.out + at * p.n_out + col0 + 8 * q + 4 * half) = make_float4(f[4 * q], f[4 * q + 1], f[4 * q + 2], f[4 * q + 3]);
+  } else {
+    // quads 2 s and 2 s + 1: the lower lane takes all eight columns of the first, the upper one of the second
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const unsigned a0 = f2bf_pair(f[8 * s], f[8 * s + 1]), a1 = f2bf_pair(f[8 * s + 2], f[8 * s + 3]);
+      const unsigned b0 = f2bf_pair(f[8 * s + 4], f[8 * s + 5]), b1 = f2bf_pair(f[8 * s + 6], f[8 * s + 7]);
+      const unsigned g0 = from_lane_xor<32>(half ? a0 : b0, lane), g1 = from_lane_xor<32>(half ? a1 : b1, lane);
+      const uint4 v = half ? make_uint4(g0, g1, b0, b1) : make_uint4(a0, a1, g0, g1);
+      if (live) *(uint4*)((bf16_t*)p.out + at * p.n_out + col0 + 16 * s + 8 * half) = v;
+    }
+  }
+}
+
+// MT x 32 rows, 4 wavefronts side by side with NS x 32 columns each.
+//
+// Weights go from memory to registers as they lie there (1 KB per instruction operand, whole lines), each wavefront its own columns'.
+// Rows go straight to the LDS in chunks of 256 inputs, three stages: while chunk c is multiplied, chunk c + 1 has landed or is about
+// to and chunk c + 2 is requested.  A chunk's step: the eight (MT NS) instructions of 64 inputs, between them the LDS reads of the next
+// step's fragments, behind them the next chunk's weights of the same step, into the registers that have just been read.
+template <int MT, int NS, int EPI>
+__global__ __launch_bounds__(256, 2) void mx_product_kernel(MxProduct p) {
+  constexpr int BM = MT * 32, STRIPS = 4 * NS, STAGES = 3;
+  constexpr unsigned CODES = BM * 128, STAGE = CODES + 1024;     // bytes; 256 dwords of scales (past row BM: zeros)
+  __shared__ uint4 ring[STAGES * STAGE / 16];
+  const unsigned ring_at = lds_address(ring);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const MxTile t = mx_tile<BM, STRIPS>(p);
+  if (!t.valid) return;
+  const int strips = p.n_out / 32, strip0 = t.strip0 + wave * NS;
   const int steps = p.n_in / MX_STEP, chunks = (steps + 3) / 4;
   const unsigned row_bytes = (unsigned)p.n_in / 2, scale_bytes = (unsigned)chunks * 8;
-  const auto ba = scalar_buffer((size_t)p.codes + (size_t)m0 * row_bytes, (size_t)m_rows * row_bytes);
-  const auto bs = scalar_buffer((size_t)p.scales + (size_t)m0 * scale_bytes, (size_t)m_rows * scale_bytes);
+  const auto ba = scalar_buffer((size_t)p.codes + (size_t)t.m0 * row_bytes, (size_t)t.m_rows * row_bytes);
+  const auto bs = scalar_buffer((size_t)p.scales + (size_t)t.m0 * scale_bytes, (size_t)t.m_rows * scale_bytes);
   const size_t scales_at = (size_t)p.groups * p.n_in * p.n_out / 2;
   __amdgpu_buffer_rsrc_t bw[NS], bws[NS];
 #pragma unroll
   for (int j = 0; j < NS; ++j) {
     const bool there = strip0 + j < strips;   // past the last column: empty ranges, zeros
-    const size_t strip = (size_t)group * strips + (there ? strip0 + j : 0);
+    const size_t strip = (size_t)t.group * strips + (there ? strip0 + j : 0);
     bw[j] = scalar_buffer((size_t)p.packed + strip * steps * 1024, there ? (size_t)steps * 1024 : 0);
     bws[j] = scalar_buffer((size_t)p.packed + scales_at + strip * chunks * 256, there ? (size_t)chunks * 256 : 0);
   }
 
-  q4_t ra[PIECES], rw[2][NS][4];
-  unsigned ras = 0, rws[2][NS];
-  auto load_a = [&](int chunk) {
+  // LDS place q (16 bytes) of a stage: row q / 8, piece (q % 8) ^ (row / 2 % 8) of it: 16 consecutive rows at one piece lie on all banks
+  constexpr int DMA = MT;                   // 16-byte requests of a lane per chunk, 32 rows each
+  const unsigned swizzle = (threadIdx.x >> 4) & 7;
+  const unsigned a_off = (threadIdx.x >> 3) * row_bytes + ((threadIdx.x & 7) ^ swizzle) * 16u, a_pass = 32u * row_bytes;
+  const unsigned s_off = (threadIdx.x >> 1) * scale_bytes + (threadIdx.x & 1) * 4u;
+  // Past the last chunk: out of range, zeros that nobody reads.  (Requested all the same: with a branch in the loop the compiler moves
+  // the matrix instructions in front of it, which it takes for arithmetic like any other, behind it, and keeps their operands.)
+  auto request = [&](int chunk, unsigned stage) {
+    const unsigned at = chunk < chunks ? 0u : 0x80000000u;
+#if defined(__HIP_DEVICE_COMPILE__)
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-      const int q = i * 256 + threadIdx.x;
-      ra[i] = __builtin_amdgcn_raw_buffer_load_b128(ba, (unsigned)(q >> 3) * row_bytes + (unsigned)chunk * 128u + (unsigned)(q & 7) * 16u, 0, 0);
-    }
-    if (threadIdx.x < BM * 2) ras = __builtin_amdgcn_raw_buffer_load_b32(bs, (unsigned)(threadIdx.x >> 1) * scale_bytes + (unsigned)chunk * 8u + (threadIdx.x & 1) * 4u, 0, 0);
+    for (int i = 0; i < DMA; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(ba, (__attribute__((address_space(3))) void*)(ring + stage / 16 + i * 256 + wave * 64), 16,
+                                               (a_off + i * a_pass + (unsigned)chunk * 128u) | at, 0, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(bs, (__attribute__((address_space(3))) void*)(ring + stage / 16 + CODES / 16 + wave * 16), 4,
+                                             (s_off + (unsigned)chunk * 8u) | at, 0, 0, 0);
+#endif
+    asm volatile("" ::: "memory");
   };
-  auto store_a = [&](int buf) {
+  u32x4_t w[NS][4], fa[2][MT];
+  unsigned ws[NS], as[MT], ws_next[NS], as_next[MT];
+  const unsigned w_off = (unsigned)lane * 16u, ws_off = (unsigned)lane * 4u;
+  auto load_w = [&](int chunk, auto ks) {
+    constexpr int J = decltype(ks)::value;
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-      const int q = i * 256 + threadIdx.x;
-      a_codes[buf][piece_at(q >> 3, q & 7)] = make_uint4(ra[i].x, ra[i].y, ra[i].z, ra[i].w);
-    }
-    if (threadIdx.x < BM * 2) a_scales[buf][threadIdx.x] = ras;
+    for (int j = 0; j < NS; ++j) w[j][J] = __builtin_amdgcn_raw_buffer_load_b128(bw[j], (unsigned)(chunk * 4 + J) * 1024u + w_off, 0, 0);
   };
-  auto load_w = [&](int chunk, auto buf) {
-    constexpr int b = decltype(buf)::value;
+  auto load_ws = [&](int chunk) {
 #pragma unroll
-    for (int j = 0; j < NS; ++j) {
-#pragma unroll
-      for (int ks = 0; ks < 4; ++ks) rw[b][j][ks] = __builtin_amdgcn_raw_buffer_load_b128(bw[j], (unsigned)(chunk * 4 + ks) * 1024u + (unsigned)lane * 16u, 0, 0);
-      rws[b][j] = __builtin_amdgcn_raw_buffer_load_b32(bws[j], (unsigned)chunk * 256u + (unsigned)lane * 4u, 0, 0);
-    }
+    for (int j = 0; j < NS; ++j) ws_next[j] = __builtin_amdgcn_raw_buffer_load_b32(bws[j], (unsigned)chunk * 256u + ws_off, 0, 0);
+  };
+  const unsigned fa_at = ring_at + (unsigned)(lane & 31) * 128u + (((unsigned)lane >> 5) ^ (((unsigned)lane >> 1) & 7)) * 16u;
+  const unsigned as_at = ring_at + CODES + (unsigned)(lane & 31) * 8u + ((unsigned)lane >> 5) * 4u;
+  auto read_a = [&](auto n, auto ks, unsigned stage) {   // fragment n of step ks
+    constexpr int i = decltype(n)::value, J = decltype(ks)::value;
+    lds_read_b128<i * 4096>((fa_at ^ (J * 32)) + stage, fa[J & 1][i]);
+  };
+  auto read_scales = [&](unsigned stage) {
+    static_for<0, MT>([&](auto n) { lds_read_b32<decltype(n)::value * 256>(as_at + stage, as_next[decltype(n)::value]); });
   };
   f32x16_t acc[MT][NS];
 #pragma unroll
   for (int i = 0; i < MT; ++i)
 #pragma unroll
-    for (int j = 0; j < NS; ++j)
+    for (int j = 0; j < NS; ++j) acc[i][j] = f32x16_t{0};
+  auto multiply = [&](auto n, auto ks) {
+    constexpr int i = decltype(n)::value / NS, j = decltype(n)::value % NS, J = decltype(ks)::value;
+    acc[i][j] = mx_mfma<J>(w[j][J], ws[j], fa[J & 1][i], as[i], acc[i][j]);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto arrived = [&](auto ks) {   // the fragments of a step, and at a chunk's first step its scales
+    constexpr int J = decltype(ks)::value;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
-      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
-  auto step = [&](int buf, auto wbuf, auto ks, const unsigned (&as)[MT]) {
-    constexpr int b = decltype(wbuf)::value, J = decltype(ks)::value;
+    for (int i = 0; i < MT; ++i) hold(fa[J & 1][i]);
+    if constexpr (J == 0) {
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      const uint4 q = a_codes[buf][piece_at(i * 32 + (lane & 31), 2 * J + (lane >> 5))];
-      const q4_t a = {q.x, q.y, q.z, q.w};
+      for (int i = 0; i < MT; ++i) {
+        hold(as_next[i]);
+        as[i] = as_next[i];
+      }
 #pragma unroll
-      for (int j = 0; j < NS; ++j) acc[i][j] = mx_mfma<J>(rw[b][j][J], rws[b][j], a, as[i], acc[i][j]);
+      for (int j = 0; j < NS; ++j) ws[j] = ws_next[j];
     }
   };
-  auto compute = [&](int chunk, int buf, auto wbuf) {
-    unsigned as[MT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i) as[i] = a_scales[buf][(i * 32 + (lane & 31)) * 2 + (lane >> 5)];
-    const int left = steps - chunk * 4;   // instructions past the last input are left out
-    step(buf, wbuf, std::integral_constant<int, 0>{}, as);
-    if (left > 1) step(buf, wbuf, std::integral_constant<int, 1>{}, as);
-    if (left > 2) step(buf, wbuf, std::integral_constant<int, 2>{}, as);
-    if (left > 3) step(buf, wbuf, std::integral_constant<int, 3>{}, as);
+  // one step of 64 inputs; meanwhile the next step's fragments are read, behind step 3 the next chunk's first
+  auto step = [&](auto ks, unsigned stage, unsigned next_stage, int chunk) {
+    constexpr int J = decltype(ks)::value;
+    arrived(ks);
+    if constexpr (J == 3) {
+      // The next chunk's rows have landed: behind its requests came this chunk's weights (5 NS), all but the last of which have been
+      // used, the requests of the chunk after it (DMA + 1) and so far 4 NS of the next chunk's weights.  And everyone has read
+      // the fragments of this chunk, whose stage takes the requests of the next turn.
+      BIGMAC_WAIT_VMCNT(DMA + 1 + 4 * NS);
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      read_scales(next_stage);
+    }
+    static_for<0, MT * NS>([&](auto n) {
+      multiply(n, ks);
+      if constexpr (decltype(n)::value < MT) {
+        if constexpr (J < 3) read_a(n, std::integral_constant<int, J + 1>{}, stage);
+        else read_a(n, std::integral_constant<int, 0>{}, next_stage);
+      }
+    });
+    load_w(chunk + 1, ks);
+    if constexpr (J == 0) load_ws(chunk + 1);
+    asm volatile("" ::: "memory");
   };
-  constexpr std::integral_constant<int, 0> B0{};
-  constexpr std::integral_constant<int, 1> B1{};
-  load_a(0);
-  load_w(0, B0);
-  store_a(0);
-  __syncthreads();
-  for (int c = 0; c < chunks; c += 2) {   // (loads past the last chunk are out of range: zeros)
-    load_a(c + 1);
-    load_w(c + 1, B1);
-    compute(c, 0, B0);
-    if (c + 1 >= chunks) break;
-    store_a(1);
-    __syncthreads();
-    load_a(c + 2);
-    load_w(c + 2, B0);
-    compute(c + 1, 1, B1);
-    store_a(0);
-    __syncthreads();
+  constexpr std::integral_constant<int, 0> I0{};
+  constexpr std::integral_constant<int, 1> I1{};
+  constexpr std::integral_constant<int, 2> I2{};
+  constexpr std::integral_constant<int, 3> I3{};
+  request(0, 0);
+  request(1, STAGE);
+  load_ws(0);
+  load_w(0, I0);
+  load_w(0, I1);
+  load_w(0, I2);
+  load_w(0, I3);
+  asm volatile("" ::: "memory");
+  BIGMAC_WAIT_VMCNT(DMA + 1 + 5 * NS);   // chunk 0 (younger: chunk 1's requests, the weights)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  read_scales(0);
+  static_for<0, MT>([&](auto n) { read_a(n, I0, 0); });
+  const int whole = steps / 4;              // chunks of four steps
+  unsigned stage = 0;
+#pragma clang loop unroll(disable)
+  for (int c = 0; c < whole; ++c) {
+    const unsigned next = stage + STAGE == STAGES * STAGE ? 0 : stage + STAGE, after = next + STAGE == STAGES * STAGE ? 0 : next + STAGE;
+    request(c + 2, after);
+    step(I0, stage, next, c);
+    step(I1, stage, next, c);
+    step(I2, stage, next, c);
+    step(I3, stage, next, c);
+    stage = next;
+  }
+  // one to three steps more; the fragments of the first are on their way (of a chunk that is not there: zeros or old ones, not used)
+  const int left = steps - whole * 4;
+  arrived(I0);
+  if (left > 0) {
+    static_for<0, MT * NS>([&](auto n) { multiply(n, I0); });
+    auto one = [&](auto ks) {
+      static_for<0, MT>([&](auto n) { read_a(n, ks, stage); });
+      arrived(ks);
+      static_for<0, MT * NS>([&](auto n) { multiply(n, ks); });
+    };
+    if (left > 1) one(I1);
+    if (left > 2) one(I2);
   }
 
-  // lane l: row l % 32 of a sub-tile, columns 8 q + 4 (l / 32) + 0 .. 3 of a strip in values 4 q .. 4 q + 3
-  const int half = lane >> 5;
 #pragma unroll
   for (int j = 0; j < NS; ++j) {
     if (strip0 + j >= strips) break;
@@ -157,45 +309,14 @@ __global__ __launch_bounds__(256, 2) void mx_product_kernel(MxProduct p) {
     if (p.bias)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const uint2 b = *(const uint2*)(p.bias + (size_t)group * p.n_out + col0 + 8 * q + 4 * half);
+        const uint2 b = *(const uint2*)(p.bias + (size_t)t.group * p.n_out + col0 + 8 * q + 4 * (lane >> 5));
         bias[4 * q] = __uint_as_float(b.x << 16); bias[4 * q + 1] = __uint_as_float(b.x & 0xFFFF0000u);
         bias[4 * q + 2] = __uint_as_float(b.y << 16); bias[4 * q + 3] = __uint_as_float(b.y & 0xFFFF0000u);
       }
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
       const int row = i * 32 + (lane & 31);
-      const bool live = row < m_rows;
-      const size_t at = (size_t)(m0 + row);
-      float f[16];
-#pragma unroll
-      for (int v = 0; v < 16; ++v) f[v] = acc[i][j][v] + bias[v];
-      if (EPI == MX_GELU_CODES) {
-        unsigned top = 0;
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          f[v] = gelu_f(f[v]);
-          top = max(top, __float_as_uint(f[v]) & 0x7FFFFFFFu);
-        }
-        top = max(top, from_lane_xor<32>(top, lane));
-        const unsigned byte = mx_scale_byte(top);
-        const unsigned lo = mx_codes8(f, byte), hi = mx_codes8(f + 8, byte);   // halfword q: this lane's four columns of quad q
-        // the lower lane puts columns 0 .. 15 together, the upper one 16 .. 31: one exchange
-        const unsigned got = from_lane_xor<32>(half ? lo : hi, lane);
-        const unsigned mine = half ? hi : lo;
-        const unsigned even = half ? got : mine, odd = half ? mine : got;      // quads of the lower lane, of the upper lane
-        if (live) {
-          *(uint2*)((uint8_t*)p.out + at * (p.n_out / 2) + col0 / 2 + 8 * half) =
-              make_uint2((even & 0xFFFFu) | (odd << 16), (even >> 16) | (odd & 0xFFFF0000u));
-          if (!half) p.out_scales[at * ((p.n_out + MX_CHUNK - 1) / MX_CHUNK * 8) + mx_scale_at((unsigned)col0 / 32)] = (uint8_t)byte;
-        }
-      } else if (live) {
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const size_t to = at * p.n_out + col0 + 8 * q + 4 * half;
-          if (EPI == MX_STORE_F32) *(float4*)((float*)p.out + to) = make_float4(f[4 * q], f[4 * q + 1], f[4 * q + 2], f[4 * q + 3]);
-          else *(uint2*)((bf16_t*)p.out + to) = make_uint2(f2bf_pair(f[4 * q], f[4 * q + 1]), f2bf_pair(f[4 * q + 2], f[4 * q + 3]));
-        }
-      }
+      mx_store<EPI>(p, acc[i][j], bias, p.bias != nullptr, t.m0 + row, row < t.m_rows, col0, lane);
     }
   }
 }
