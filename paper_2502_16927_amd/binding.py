@@ -194,8 +194,8 @@ def _nbytes(t):
 
 
 def _stream(stream):
-    if stream is None:
-        stream = torch.cuda.current_stream().cuda_stream
+    if stream is None:      # the current stream's handle without a Stream object around it (2 us of a 7 us call)
+        stream = torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return stream
 
 

@@ -7,7 +7,6 @@
 #include <algorithm>
 
 #include "mx.hpp"
-#include "tile_map.hpp"
 
 namespace bigmac {
 
@@ -29,12 +28,61 @@ __device__ __forceinline__ void put8(float* p, const float* f) {
 }
 __device__ __forceinline__ void put8(bf16_t* p, const float* f) { *(uint4*)p = pack_bf16x8(f); }
 
+// The tile map by one workgroup of 256 threads, up to 1024 groups: tiles in front of every group (four groups a thread, a scan over the
+// wavefronts), then each thread finds the groups of every 256th tile.
+__device__ __forceinline__ void build_mx_map(const MxMapJob& job) {
+  __shared__ int before[1025], wave_total[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g0 = threadIdx.x * 4;
+  int count[4], sum = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int g = g0 + i;
+    count[i] = g < job.groups ? (job.offsets[g + 1] - job.offsets[g] + job.tile_rows - 1) / job.tile_rows : 0;
+    sum += count[i];
+  }
+  int upto = sum;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int o = __shfl_up(upto, d, 64);
+    if (lane >= d) upto += o;
+  }
+  if (lane == 63) wave_total[wave] = upto;
+  __syncthreads();
+  int at = upto - sum;
+  for (int w = 0; w < wave; ++w) at += wave_total[w];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    before[g0 + i] = at;
+    at += count[i];
+  }
+  if (threadIdx.x == 255) {
+    before[1024] = at;
+    job.map[0] = at;
+  }
+  __syncthreads();
+  const int tiles = before[1024];
+  for (int i = threadIdx.x; i < tiles; i += 256) {
+    int lo = 0, hi = job.groups;           // the last group that starts at or in front of tile i: groups without rows start where the next one does
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (before[mid] <= i) lo = mid;
+      else hi = mid;
+    }
+    *(int2*)(job.map + 2 + 2 * i) = make_int2(lo, job.offsets[lo] + (i - before[lo]) * job.tile_rows);
+  }
+}
+__global__ __launch_bounds__(256) void mx_map_kernel(MxMapJob job) { build_mx_map(job); }
+
 constexpr int ROW_TURNS = 4;   // rows a thread takes
 
 // 1 << log_tx threads side by side on a row, the others on further rows
 template <typename T>
 __global__ __launch_bounds__(256) void mx_quantize_kernel(const T* __restrict__ src, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales, long rows,
-                                                          int cols, int log_tx, int scale_bytes) {
+                                                          int cols, int log_tx, int scale_bytes, MxMapJob map) {
+  if (map.map && blockIdx.x == gridDim.x - 1) {
+    build_mx_map(map);
+    return;
+  }
   const int tx = threadIdx.x & ((1 << log_tx) - 1), ty = threadIdx.x >> log_tx, rows_at_once = 256 >> log_tx;
   const int pieces = cols / 8;
   for (int p = tx; p < scale_bytes * 4; p += 1 << log_tx) {   // (a multiple of 4 pieces; past the row's end only the unused scale bytes)
@@ -211,7 +259,7 @@ int check_mx(const bigmac_mx_dims* D) {
   if (!D || D->rows < 1 || (D->out_dtype != BIGMAC_F32 && D->out_dtype != BIGMAC_BF16)) return BIGMAC_ERR_INVALID_ARG;
   return check_weights(D->groups, D->n_in, D->n_out);
 }
-size_t mx_map_bytes(int rows, int groups) { return align_up(tile_map_ints(rows, groups, 32) * 4); }   // for every tile height
+size_t mx_map_bytes(int rows, int groups) { return align_up(mx_map_ints(rows, groups) * 4); }
 
 struct FfnPlan {
   size_t x_codes, x_scales, h_codes, h_scales, map, total;
@@ -231,11 +279,13 @@ FfnPlan plan_ffn(const bigmac_dims& D) {
 
 }  // namespace
 
-int launch_mx_quantize(long rows, long cols, int dtype, const void* src, uint8_t* codes, uint8_t* scales, hipStream_t s) {
+int launch_mx_quantize(long rows, long cols, int dtype, const void* src, uint8_t* codes, uint8_t* scales, hipStream_t s, const MxMapJob* map) {
   const int scale_bytes = (int)mx_scale_bytes(cols);
   const RowGrid g = row_grid(rows, cols / 8);
-  if (dtype == BIGMAC_BF16) mx_quantize_kernel<bf16_t><<<g.blocks, 256, 0, s>>>((const bf16_t*)src, codes, scales, rows, (int)cols, g.log_tx, scale_bytes);
-  else mx_quantize_kernel<float><<<g.blocks, 256, 0, s>>>((const float*)src, codes, scales, rows, (int)cols, g.log_tx, scale_bytes);
+  const MxMapJob job = map ? *map : MxMapJob{};
+  const unsigned blocks = g.blocks + (map ? 1 : 0);
+  if (dtype == BIGMAC_BF16) mx_quantize_kernel<bf16_t><<<blocks, 256, 0, s>>>((const bf16_t*)src, codes, scales, rows, (int)cols, g.log_tx, scale_bytes, job);
+  else mx_quantize_kernel<float><<<blocks, 256, 0, s>>>((const float*)src, codes, scales, rows, (int)cols, g.log_tx, scale_bytes, job);
   BIGMAC_CHECK_LAUNCH();
   return BIGMAC_OK;
 }
@@ -319,11 +369,8 @@ int bigmac_mx_product(const bigmac_mx_dims* D, const void* codes, const void* sc
     if (ws_bytes < mx_map_bytes(D->rows, D->groups)) return BIGMAC_ERR_WORKSPACE;
     p.offsets = offsets;
     p.tile_map = (const int*)ws;
-    TileMapJobs maps{};
-    maps.tile_rows[0] = mx_tile_rows(D->rows, D->groups);
-    maps.map[0] = (int*)ws;
-    rc = launch_build_tile_map(offsets, D->groups, maps, s);
-    if (rc) return rc;
+    mx_map_kernel<<<1, 256, 0, s>>>(MxMapJob{offsets, (int*)ws, D->groups, mx_tile_rows(D->rows, D->groups)});
+    BIGMAC_CHECK_LAUNCH();
   }
   return launch_mx_product(p, s);
 }
@@ -342,16 +389,12 @@ int bigmac_mx_grouped_ffn(const bigmac_dims* D, const void* x_perm, const int32_
   hipStream_t s = (hipStream_t)stream;
   const int rows = (int)((long)D->T * D->k);
   uint8_t* base = (uint8_t*)ws;
-  TileMapJobs maps{};
-  maps.tile_rows[0] = mx_tile_rows(rows, D->N);
-  maps.map[0] = (int*)(base + plan.map);
-  rc = launch_build_tile_map(expert_offsets, D->N, maps, s);
-  if (rc) return rc;
-  rc = launch_mx_quantize(rows, W.win, BIGMAC_BF16, x_perm, base + plan.x_codes, base + plan.x_scales, s);
+  const MxMapJob map{expert_offsets, (int*)(base + plan.map), D->N, mx_tile_rows(rows, D->N)};
+  rc = launch_mx_quantize(rows, W.win, BIGMAC_BF16, x_perm, base + plan.x_codes, base + plan.x_scales, s, &map);
   if (rc) return rc;
   MxProduct p{};
   p.codes = base + plan.x_codes; p.scales = base + plan.x_scales; p.packed = (const uint8_t*)w1; p.bias = (const bf16_t*)b1;
-  p.offsets = expert_offsets; p.tile_map = maps.map[0];
+  p.offsets = expert_offsets; p.tile_map = map.map;
   p.out = base + plan.h_codes; p.out_scales = base + plan.h_scales;
   p.rows = rows; p.groups = D->N; p.n_in = W.win; p.n_out = W.hid; p.epilogue = MX_GELU_CODES;
   rc = launch_mx_product(p, s);

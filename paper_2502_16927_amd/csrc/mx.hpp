@@ -60,13 +60,21 @@ struct MxProduct {
   const uint8_t* packed;           // W: [groups] of n_in x n_out
   const bf16_t* bias;              // [groups][n_out] or NULL
   const int* offsets;              // device [groups + 1], or NULL: one group of all rows
-  const int* tile_map;             // device, with offsets: of mx_tile_rows rows (tile_map.hpp)
+  const int* tile_map;             // device, with offsets: from an MxMapJob of mx_tile_rows rows
   void* out;                       // [rows][n_out] bf16 or fp32, or codes
   uint8_t* out_scales;             // MX_GELU_CODES: of the rows of codes
   int rows, groups, n_in, n_out, epilogue;
 };
 int mx_tile_rows(int rows, int groups);
 int launch_mx_product(const MxProduct& p, hipStream_t s);
-int launch_mx_quantize(long rows, long cols, int dtype, const void* src, uint8_t* codes, uint8_t* scales, hipStream_t s);
+// The row tiles of a ragged product: map[0] = how many, then from map[2] on (group, first row) of each, groups in order
+struct MxMapJob {
+  const int* offsets;              // device [groups + 1]
+  int* map;                        // device, mx_map_ints(rows, groups); NULL: no job
+  int groups, tile_rows;
+};
+inline size_t mx_map_ints(long rows, long groups) { return 2 + 2 * ((size_t)rows / 32 + groups + 1); }   // for every tile height
+// map (optional): the tile map by a workgroup of the same launch
+int launch_mx_quantize(long rows, long cols, int dtype, const void* src, uint8_t* codes, uint8_t* scales, hipStream_t s, const MxMapJob* map = nullptr);
 
 }  // namespace bigmac

@@ -30,18 +30,18 @@ __device__ __forceinline__ void hold(T& v) { asm volatile("" : "+v"(v)); }
 template <int OFFSET>
 __device__ __forceinline__ void lds_read_b32(unsigned addr, unsigned& v) { asm volatile("ds_read_b32 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(OFFSET) : "memory"); }
 
-// GELU for 4-bit results: a polynomial of degree 6 for log2 of the normal tail (weighted least squares of |a| tail(|a|): absolute error
-// of the GELU under 8e-8, relative error of the tail under 5e-6 up to |a| = 2 and 4e-4 at 4; a step of a 4-bit value is an eighth of it and more).
-// |a| is cut off at 9, where the tail's fit is 2^-62.  fmed3 with infinity: max(a, 0) in one instruction.
+// GELU for 4-bit results: a polynomial of degree 5 for log2 of the normal tail (minimax of the tail's absolute error, of |a| times it past
+// 1: under 7e-7, so within 7e-7 of |a| and of 1; the smallest step of a 4-bit value is an eighth of it or more).  It falls without end, so |a|
+// needs no limit.  max(a, 0) on the bits as an integer: one instruction.  The vector ALU is what bounds a product with this epilogue (the
+// 131072 x 4096 hidden values of a 16384-token call: each instruction per value is 17 us).
 __device__ __forceinline__ float gelu_mx_f(float a) {
-  const float x = __builtin_amdgcn_fmed3f(fabsf(a), 0.0f, 9.0f);
-  float q = fmaf(x, 3.31598240e-05f, -7.69719801e-04f);
-  q = fmaf(x, q, 8.08210559e-03f);
-  q = fmaf(x, q, -5.34138962e-02f);
-  q = fmaf(x, q, -4.58769884e-01f);
-  q = fmaf(x, q, -1.15120198e+00f);
-  q = fmaf(x, q, -9.99993041e-01f);
-  return fmaf(-fabsf(a), __builtin_amdgcn_exp2f(q), __builtin_amdgcn_fmed3f(a, 0.0f, INFINITY));
+  const float x = fabsf(a);
+  float q = fmaf(x, -5.002595082e-04f, 7.282377832e-03f);
+  q = fmaf(x, q, -5.234324002e-02f);
+  q = fmaf(x, q, -4.594140765e-01f);
+  q = fmaf(x, q, -1.151052049e+00f);
+  q = fmaf(x, q, -1.000001856e+00f);
+  return fmaf(-x, __builtin_amdgcn_exp2f(q), __int_as_float(max(__float_as_int(a), 0)));
 }
 // largest magnitude of 16 values, NaN if one is
 __device__ __forceinline__ float top_of(const float (&f)[16]) {
@@ -72,69 +72,96 @@ __device__ __forceinline__ MxTile mx_tile(const MxProduct& p) {
   const int strips = p.n_out / 32, gx = (strips + STRIPS - 1) / STRIPS;
   const int tiles = p.offsets ? table_at(p.tile_map, 0) : (p.rows + BM - 1) / BM;
   // consecutive workgroups go to the 8 XCDs in turn: each XCD gets a run of consecutive tiles, column tiles fastest
-  const long total = (long)tiles * gx;
-  const long per_xcd = (total + 7) / 8, slot = blockIdx.x >> 3;
-  const long id = (long)(blockIdx.x & 7) * per_xcd + slot;
+  const unsigned total = (unsigned)tiles * (unsigned)gx, per_xcd = (total + 7) / 8, slot = blockIdx.x >> 3, id = (blockIdx.x & 7) * per_xcd + slot;
   t.valid = slot < per_xcd && id < total;
   if (!t.valid) return t;
-  const int tile = (int)(id / gx);
-  t.strip0 = (int)(id % gx) * STRIPS;
+  const int tile = (int)(id / (unsigned)gx);
+  t.strip0 = (int)(id % (unsigned)gx) * STRIPS;
   int m_end = p.rows;
   t.group = 0;
   t.m0 = tile * BM;
   if (p.offsets) {
-    t.group = table_at(p.tile_map, TILE_MAP_HEADER + p.groups + 2 * tile);
-    t.m0 = table_at(p.tile_map, TILE_MAP_HEADER + p.groups + 1 + 2 * tile);
+    t.group = table_at(p.tile_map, 2 + 2 * tile);
+    t.m0 = table_at(p.tile_map, 3 + 2 * tile);
     m_end = table_at(p.offsets, t.group + 1);
   }
   t.m_rows = min(m_end - t.m0, BM);
   return t;
 }
 
-// Results of a sub-tile of 32 rows x 32 columns.  Lane l: row l % 32, columns 8 q + 4 (l / 32) + 0 .. 3 in values 4 q .. 4 q + 3.
-template <int EPI>
-__device__ __forceinline__ void mx_store(const MxProduct& p, const f32x16_t& acc, const float (&bias)[16], bool biased, int row, bool live, int col0, int lane) {
+// A row of 128 bytes in the LDS as eight pieces of 16, in places that put 16 consecutive rows' equal pieces on all banks
+__device__ __forceinline__ unsigned piece_place(unsigned row, unsigned piece) { return row * 128u + (piece ^ ((row >> 1) & 7u)) * 16u; }
+
+// Results leave as whole lines.  A sub-tile of 32 x 32 lies in the lanes as: row l % 32, columns 8 q + 4 (l / 32) + 0 .. 3 in values 4 q .. 4 q + 3.
+// bf16 and fp32: through 4 KB of the wavefront's own, 32 rows x 128 bytes.  (Stored from where they lie, 32 bytes of a row at a time, they
+// were four requests a line; the 8 and 1 bytes of the 4-bit epilogue 16 and 8.)
+__device__ __forceinline__ void strip_out(char* strip, const MxProduct& p, int row0, int rows, size_t col_byte, size_t row_bytes, int lane) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const unsigned q = i * 64 + lane, row = q >> 3;
+    const uint4 v = *(const uint4*)(strip + piece_place(row, q & 7));
+    if ((int)row < rows) *(uint4*)((char*)p.out + (size_t)(row0 + (int)row) * row_bytes + col_byte + (q & 7) * 16) = v;
+  }
+}
+template <int NS>
+__device__ __forceinline__ void mx_store(const MxProduct& p, const f32x16_t (&acc)[NS], const float (&bias)[NS][16], int row0, int rows, int col0, char* strip, int lane,
+                                         std::integral_constant<int, MX_STORE_BF16>) {
+  static_assert(NS == 2, "64 columns are a line of bf16");
   const int half = lane >> 5;
-  const size_t at = (size_t)row;
-  float f[16];
 #pragma unroll
-  for (int v = 0; v < 16; ++v) f[v] = acc[v];
-  if (biased)
-#pragma unroll
-    for (int v = 0; v < 16; ++v) f[v] += bias[v];
-  if (EPI == MX_GELU_CODES) {
-#pragma unroll
-    for (int v = 0; v < 16; ++v) f[v] = gelu_mx_f(f[v]);
-    unsigned top = __float_as_uint(top_of(f));
-    top = max(top, from_lane_xor<32>(top, lane));   // (magnitudes and NaN are ordered as integers; the NaN may have its sign set: the shift below drops it)
-    top &= 0x7FFFFFFFu;
-    // the smallest scale here is 2^-126: values of a block under 2^-124 that 2^-127 would hold better
-    const unsigned byte = max(mx_scale_byte(top), 1u);
-    const unsigned lo = mx_codes8_scaled(f, byte), hi = mx_codes8_scaled(f + 8, byte);   // halfword q: this lane's four columns of quad q
-    // the lower lane puts columns 0 .. 15 together, the upper one 16 .. 31: one exchange
-    const unsigned got = from_lane_xor<32>(half ? lo : hi, lane);
-    const unsigned mine = half ? hi : lo;
-    const unsigned even = half ? got : mine, odd = half ? mine : got;      // quads of the lower lane, of the upper lane
-    if (live) {
-      *(uint2*)((uint8_t*)p.out + at * (p.n_out / 2) + col0 / 2 + 8 * half) =
-          make_uint2((even & 0xFFFFu) | (odd << 16), (even >> 16) | (odd & 0xFFFF0000u));
-      if (!half) p.out_scales[at * ((p.n_out + MX_CHUNK - 1) / MX_CHUNK * 8) + mx_scale_at((unsigned)col0 / 32)] = (uint8_t)byte;
-    }
-  } else if (EPI == MX_STORE_F32) {
-    if (live)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) *(float4*)((float*)p.out + at * p.n_out + col0 + 8 * q + 4 * half) = make_float4(f[4 * q], f[4 * q + 1], f[4 * q + 2], f[4 * q + 3]);
-  } else {
-    // quads 2 s and 2 s + 1: the lower lane takes all eight columns of the first, the upper one of the second
+  for (int j = 0; j < NS; ++j)
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      const unsigned a0 = f2bf_pair(f[8 * s], f[8 * s + 1]), a1 = f2bf_pair(f[8 * s + 2], f[8 * s + 3]);
-      const unsigned b0 = f2bf_pair(f[8 * s + 4], f[8 * s + 5]), b1 = f2bf_pair(f[8 * s + 6], f[8 * s + 7]);
-      const unsigned g0 = from_lane_xor<32>(half ? a0 : b0, lane), g1 = from_lane_xor<32>(half ? a1 : b1, lane);
-      const uint4 v = half ? make_uint4(g0, g1, b0, b1) : make_uint4(a0, a1, g0, g1);
-      if (live) *(uint4*)((bf16_t*)p.out + at * p.n_out + col0 + 16 * s + 8 * half) = v;
+      float f[8];
+#pragma unroll
+      for (int v = 0; v < 8; ++v) f[v] = acc[j][8 * s + v] + bias[j][8 * s + v];
+      // quads 2 s and 2 s + 1: the lower lane takes all eight columns of the first, the upper one of the second
+      const auto r0 = __builtin_amdgcn_permlane32_swap(f2bf_pair(f[0], f[1]), f2bf_pair(f[4], f[5]), false, false);
+      const auto r1 = __builtin_amdgcn_permlane32_swap(f2bf_pair(f[2], f[3]), f2bf_pair(f[6], f[7]), false, false);
+      *(uint4*)(strip + piece_place(lane & 31, j * 4 + s * 2 + half)) = make_uint4(r0[0], r1[0], r0[1], r1[1]);
     }
+  strip_out(strip, p, row0, rows, (size_t)col0 * 2, (size_t)p.n_out * 2, lane);
+}
+template <int NS>
+__device__ __forceinline__ void mx_store(const MxProduct& p, const f32x16_t (&acc)[NS], const float (&bias)[NS][16], int row0, int rows, int col0, char* strip, int lane,
+                                         std::integral_constant<int, MX_STORE_F32>) {
+#pragma unroll
+  for (int j = 0; j < NS; ++j) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      *(float4*)(strip + piece_place(lane & 31, 2 * q + (lane >> 5))) = make_float4(acc[j][4 * q] + bias[j][4 * q], acc[j][4 * q + 1] + bias[j][4 * q + 1],
+                                                                                    acc[j][4 * q + 2] + bias[j][4 * q + 2], acc[j][4 * q + 3] + bias[j][4 * q + 3]);
+    strip_out(strip, p, row0, rows, (size_t)(col0 + 32 * j) * 4, (size_t)p.n_out * 4, lane);
   }
+}
+// GELU and 4 bits: 32 rows x 64 columns of a wavefront into the workgroup's [rows][256 columns] of codes (128 bytes a row) and [rows][8] of scales
+template <int NS>
+__device__ __forceinline__ void mx_gelu_codes(const f32x16_t (&acc)[NS], const float (&bias)[NS][16], bool biased, char* codes, uint8_t* scales, int row0, int wave, int lane) {
+  static_assert(NS == 2, "a wavefront's 64 columns are two blocks");
+  uint2 half_block[NS];   // lower lane: columns 0 .. 15 of a block, upper lane: 16 .. 31
+#pragma unroll
+  for (int j = 0; j < NS; ++j) {
+    float f[16];
+#pragma unroll
+    for (int v = 0; v < 16; ++v) f[v] = acc[j][v];
+    if (biased)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) f[v] += bias[j][v];
+#pragma unroll
+    for (int v = 0; v < 16; ++v) f[v] = gelu_mx_f(f[v]);
+    const unsigned mine = __float_as_uint(top_of(f));
+    const auto both = __builtin_amdgcn_permlane32_swap(mine, mine, false, false);
+    // the smallest scale here is 2^-126: values of a block under 2^-124 that 2^-127 would hold better
+    const unsigned byte = max(mx_scale_byte(max(both[0], both[1]) & 0x7FFFFFFFu), 1u);   // (a NaN is the largest, with its sign or without)
+    // halfword q: this lane's four columns of quad q; lower lane: the lower and the upper lane's of quads 0 and 1, upper lane: of quads 2 and 3
+    const auto r = __builtin_amdgcn_permlane32_swap(mx_codes8_scaled(f, byte), mx_codes8_scaled(f + 8, byte), false, false);
+    half_block[j] = make_uint2((r[0] & 0xFFFFu) | (r[1] << 16), (r[0] >> 16) | (r[1] & 0xFFFF0000u));
+    if (lane < 32) scales[(row0 + lane) * 8 + j * 4 + wave] = (uint8_t)byte;
+  }
+  // whole blocks: the first in the lower lane, the second in the upper
+  const auto x = __builtin_amdgcn_permlane32_swap(half_block[0].x, half_block[1].x, false, false);
+  const auto y = __builtin_amdgcn_permlane32_swap(half_block[0].y, half_block[1].y, false, false);
+  *(uint4*)(codes + piece_place(row0 + (lane & 31), wave * 2 + (lane >> 5))) = make_uint4(x[0], y[0], x[1], y[1]);
 }
 
 // MT x 32 rows, 4 wavefronts side by side with NS x 32 columns each.
@@ -144,10 +171,13 @@ __device__ __forceinline__ void mx_store(const MxProduct& p, const f32x16_t& acc
 // to and chunk c + 2 is requested.  A chunk's step: the eight (MT NS) instructions of 64 inputs, between them the LDS reads of the next
 // step's fragments, behind them the next chunk's weights of the same step, into the registers that have just been read.
 template <int MT, int NS, int EPI>
-__global__ __launch_bounds__(256, 2) void mx_product_kernel(MxProduct p) {
+__global__ __launch_bounds__(256, MT * NS == 8 ? 2 : 3) void mx_product_kernel(MxProduct p) {
   constexpr int BM = MT * 32, STRIPS = 4 * NS, STAGES = 3;
   constexpr unsigned CODES = BM * 128, STAGE = CODES + 1024;     // bytes; 256 dwords of scales (past row BM: zeros)
   __shared__ uint4 ring[STAGES * STAGE / 16];
+  constexpr int OUT = EPI == MX_GELU_CODES ? BM * 128 : 4 * 4096;
+  __shared__ uint4 staging[OUT / 16];
+  __shared__ __align__(16) uint8_t out_scales[EPI == MX_GELU_CODES ? BM * 8 : 8];
   const unsigned ring_at = lds_address(ring);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const MxTile t = mx_tile<BM, STRIPS>(p);
@@ -299,25 +329,45 @@ __global__ __launch_bounds__(256, 2) void mx_product_kernel(MxProduct p) {
     if (left > 2) one(I2);
   }
 
+  const bool there = strip0 < strips;       // (strips are whole pairs)
+  float bias[NS][16];
 #pragma unroll
-  for (int j = 0; j < NS; ++j) {
-    if (strip0 + j >= strips) break;
-    const int col0 = (strip0 + j) * 32;
-    float bias[16];
+  for (int j = 0; j < NS; ++j)
 #pragma unroll
-    for (int v = 0; v < 16; ++v) bias[v] = 0.0f;
-    if (p.bias)
+    for (int v = 0; v < 16; ++v) bias[j][v] = 0.0f;
+  if (p.bias && there)
+#pragma unroll
+    for (int j = 0; j < NS; ++j)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const uint2 b = *(const uint2*)(p.bias + (size_t)t.group * p.n_out + col0 + 8 * q + 4 * (lane >> 5));
-        bias[4 * q] = __uint_as_float(b.x << 16); bias[4 * q + 1] = __uint_as_float(b.x & 0xFFFF0000u);
-        bias[4 * q + 2] = __uint_as_float(b.y << 16); bias[4 * q + 3] = __uint_as_float(b.y & 0xFFFF0000u);
+        const uint2 b = *(const uint2*)(p.bias + (size_t)t.group * p.n_out + (strip0 + j) * 32 + 8 * q + 4 * (lane >> 5));
+        bias[j][4 * q] = __uint_as_float(b.x << 16); bias[j][4 * q + 1] = __uint_as_float(b.x & 0xFFFF0000u);
+        bias[j][4 * q + 2] = __uint_as_float(b.y << 16); bias[j][4 * q + 3] = __uint_as_float(b.y & 0xFFFF0000u);
       }
+  if constexpr (EPI == MX_GELU_CODES) {
+    if (there) {
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+        if (i * 32 < t.m_rows) mx_gelu_codes<NS>(acc[i], bias, p.bias != nullptr, (char*)staging, out_scales, i * 32, wave, lane);
+    }
+    __syncthreads();
+    const size_t row_out = (size_t)p.n_out / 2, scales_out = (size_t)((p.n_out + MX_CHUNK - 1) / MX_CHUNK) * 8;
+    const int pieces = min(8, strips - t.strip0);   // of the workgroup's 256 columns, 32 each
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-      const int row = i * 32 + (lane & 31);
-      mx_store<EPI>(p, acc[i][j], bias, p.bias != nullptr, t.m0 + row, row < t.m_rows, col0, lane);
+      const unsigned q = i * 256 + threadIdx.x, row = q >> 3, piece = q & 7;
+      const uint4 v = *(const uint4*)((const char*)staging + piece_place(row, piece));
+      if ((int)row < t.m_rows && (int)piece < pieces) *(uint4*)((uint8_t*)p.out + (size_t)(t.m0 + (int)row) * row_out + (size_t)t.strip0 * 16 + piece * 16) = v;
     }
+    // (bytes of blocks past the last column are whatever the LDS held: nobody reads them)
+    if ((int)threadIdx.x < t.m_rows)
+      *(uint2*)(p.out_scales + (size_t)(t.m0 + (int)threadIdx.x) * scales_out + t.strip0) = *(const uint2*)(out_scales + threadIdx.x * 8);
+  } else {
+    if (!there) return;
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+      if (i * 32 < t.m_rows)
+        mx_store<NS>(p, acc[i], bias, t.m0 + i * 32, t.m_rows - i * 32, strip0 * 32, (char*)staging + wave * 4096, lane, std::integral_constant<int, EPI>{});
   }
 }
 
@@ -326,7 +376,7 @@ int launch_of(const MxProduct& p, hipStream_t s) {
   const long tiles = p.offsets ? (long)p.rows / (MT * 32) + p.groups : ((long)p.rows + MT * 32 - 1) / (MT * 32);
   const long gx = (p.n_out / 32 + 4 * NS - 1) / (4 * NS);
   const long blocks = (tiles * gx + 7) / 8 * 8;
-  if (blocks > 0x7FFFFFFFl / 256 * 255) return BIGMAC_ERR_TOO_LARGE;
+  if (blocks > 0x3FFFFFFFl) return BIGMAC_ERR_TOO_LARGE;
   const dim3 grid((unsigned)blocks);
   if (p.epilogue == MX_GELU_CODES) mx_product_kernel<MT, NS, MX_GELU_CODES><<<grid, 256, 0, s>>>(p);
   else if (p.epilogue == MX_STORE_F32) mx_product_kernel<MT, NS, MX_STORE_F32><<<grid, 256, 0, s>>>(p);

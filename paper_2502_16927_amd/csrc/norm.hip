@@ -410,8 +410,8 @@ __global__ __launch_bounds__((RowShape<W, NV>::THREADS)) void norm_backward_kern
     }
 }
 
-// The workgroups' sums of a vector, 64 columns per workgroup: 16 groups of threads each add every 16th workgroup's, 4 columns a
-// thread, then the groups' are added in order.
+// The workgroups' sums of a vector, 16 columns per workgroup: 64 groups of threads each add every 64th workgroup's, 4 columns a thread,
+// then the groups' are added in order, four and four and then sixteen.  (64 columns per workgroup: 16 x 2 of them at 1024 columns, 13.8 us.)
 struct NormReduce {
   const float* part;
   const float *post_w, *post_b, *channel_gate;   // channel gate: NULL if the gate is none
@@ -419,15 +419,17 @@ struct NormReduce {
   int workgroups, vectors, d, pre, post, beta;
 };
 __global__ __launch_bounds__(256) void norm_reduce_kernel(NormReduce p) {
-  __shared__ float4 box[2][16][16];
-  const int quad = threadIdx.x & 15, group = threadIdx.x >> 4;
-  const int col = blockIdx.x * 64 + quad * 4;
+  __shared__ float4 box[2][64][4];
+  __shared__ float fours[2][16][16];
+  const int quad = threadIdx.x & 3, group = threadIdx.x >> 2;
+  const int col = blockIdx.x * 16 + quad * 4;
   const bool post = p.pre ? blockIdx.y == 1 : true;      // which side's vectors
   const bool bias = p.vectors == 2 * (p.pre + p.post);
-  const int k0 = post && p.pre ? 1 : 0, k1 = bias ? p.pre + p.post + k0 : -1;
+  const int k0 = post && p.pre ? 1 : 0, k1 = p.pre + p.post + k0;
   float4 s0 = make_float4(0.f, 0.f, 0.f, 0.f), s1 = s0;
   if (col < p.d)
-    for (int g = group; g < p.workgroups; g += 16) {
+#pragma unroll 4
+    for (int g = group; g < p.workgroups; g += 64) {
       const float4 a = *(const float4*)(p.part + ((size_t)g * p.vectors + k0) * p.d + col);
       s0.x += a.x; s0.y += a.y; s0.z += a.z; s0.w += a.w;
       if (bias) {
@@ -438,15 +440,23 @@ __global__ __launch_bounds__(256) void norm_reduce_kernel(NormReduce p) {
   box[0][group][quad] = s0;
   box[1][group][quad] = s1;
   __syncthreads();
-  const int c = threadIdx.x;                              // one column a thread from here on
-  if (c >= 64 || blockIdx.x * 64 + c >= p.d) return;
+  const int c = threadIdx.x & 15, part = threadIdx.x >> 4;   // one column a thread from here on
+#pragma unroll
+  for (int v = 0; v < 2; ++v) {
+    float t = 0.0f;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) t += ((const float*)box[v][part * 4 + g])[c];
+    fours[v][part][c] = t;
+  }
+  __syncthreads();
+  if (part > 0 || blockIdx.x * 16 + c >= p.d) return;
   float t0 = 0.0f, t1 = 0.0f;
 #pragma unroll
   for (int g = 0; g < 16; ++g) {
-    t0 += ((const float*)box[0][g])[c];
-    t1 += ((const float*)box[1][g])[c];
+    t0 += fours[0][g][c];
+    t1 += fours[1][g][c];
   }
-  const int n = blockIdx.x * 64 + c;
+  const int n = blockIdx.x * 16 + c;
   auto put = [&](float* to, float v) { if (to) to[n] = p.beta ? to[n] + v : v; };
   if (!post) {
     put(p.d_pre_w, t0);
@@ -609,7 +619,7 @@ int bigmac_norm_backward(const bigmac_norm_dims* D, const bigmac_norm_params* P,
   r.d_gate = D->gate == BIGMAC_GATE_CHANNEL ? (float*)d_gate : nullptr;
   r.workgroups = workgroups; r.vectors = vectors; r.d = D->d; r.pre = pre; r.post = post;
   r.beta = D->parts & BIGMAC_NORM_ACCUMULATE ? 1 : 0;
-  norm_reduce_kernel<<<dim3((D->d + 63) / 64, (pre ? 1 : 0) + (post ? 1 : 0)), 256, 0, s>>>(r);
+  norm_reduce_kernel<<<dim3((D->d + 15) / 16, (pre ? 1 : 0) + (post ? 1 : 0)), 256, 0, s>>>(r);
   BIGMAC_CHECK_LAUNCH();
   return BIGMAC_OK;
 }
