@@ -157,11 +157,11 @@ __device__ __forceinline__ void put4(float* p, const float* f) { *(float4*)p = m
 __device__ __forceinline__ void put4(bf16_t* p, const float* f) { *(uint2*)p = make_uint2(f2bf_pair(f[0], f[1]), f2bf_pair(f[2], f[3])); }
 
 template <typename T>
-__global__ __launch_bounds__(256) void mx_pack_kernel(const T* __restrict__ w, uint8_t* __restrict__ packed, size_t scales_at, long groups, int n_in, int n_out) {
+__global__ __launch_bounds__(256) void mx_pack_kernel(const T* __restrict__ w, uint8_t* __restrict__ packed, long groups, int n_in, int n_out) {
   const PackPlace t = pack_place(groups, n_in, n_out);
   if (!t.any) return;
-  const int steps = n_in / MX_STEP, chunks = (n_in + MX_CHUNK - 1) / MX_CHUNK, strips = n_out / 32;
-  const long strip = t.group * strips + t.col / 32;
+  const int steps = n_in / MX_STEP;
+  const size_t strip = (size_t)(t.group * (n_out / 32) + t.col / 32) * mx_strip_bytes(n_in);
   const int lane = t.half * 32 + t.col % 32;
   unsigned bytes[4] = {0, 0, 0, 0};
 #pragma unroll 1
@@ -177,7 +177,7 @@ __global__ __launch_bounds__(256) void mx_pack_kernel(const T* __restrict__ w, u
 #pragma unroll
       for (int c = 0; c < 4; ++c) f[c][k] = v[c];
     }
-    uint4* to = (uint4*)(packed + (strip * steps + step) * 1024) + lane;
+    uint4* to = (uint4*)(packed + strip + (size_t)step * 1024) + lane;
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       unsigned top = 0;
@@ -188,24 +188,24 @@ __global__ __launch_bounds__(256) void mx_pack_kernel(const T* __restrict__ w, u
       bytes[c] |= byte << (8 * j);
     }
   }
-  *(uint4*)(packed + scales_at + (strip * chunks + t.chunk) * 256 + lane * 4) = make_uint4(bytes[0], bytes[1], bytes[2], bytes[3]);
+  *(uint4*)(packed + strip + (size_t)steps * 1024 + t.chunk * 256 + lane * 4) = make_uint4(bytes[0], bytes[1], bytes[2], bytes[3]);
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void mx_unpack_kernel(const uint8_t* __restrict__ packed, size_t scales_at, T* __restrict__ w, long groups, int n_in, int n_out) {
+__global__ __launch_bounds__(256) void mx_unpack_kernel(const uint8_t* __restrict__ packed, T* __restrict__ w, long groups, int n_in, int n_out) {
   const PackPlace t = pack_place(groups, n_in, n_out);
   if (!t.any) return;
-  const int steps = n_in / MX_STEP, chunks = (n_in + MX_CHUNK - 1) / MX_CHUNK, strips = n_out / 32;
-  const long strip = t.group * strips + t.col / 32;
+  const int steps = n_in / MX_STEP;
+  const size_t strip = (size_t)(t.group * (n_out / 32) + t.col / 32) * mx_strip_bytes(n_in);
   const int lane = t.half * 32 + t.col % 32;
-  const uint4 b = *(const uint4*)(packed + scales_at + (strip * chunks + t.chunk) * 256 + lane * 4);
+  const uint4 b = *(const uint4*)(packed + strip + (size_t)steps * 1024 + t.chunk * 256 + lane * 4);
   const unsigned bytes[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll 1
   for (int j = 0; j < 4; ++j) {
     const int step = t.chunk * 4 + j;
     if (step >= steps) break;
     T* to = w + (t.group * n_in + step * MX_STEP + t.half * MX_BLOCK) * n_out + t.col;
-    const uint4* from = (const uint4*)(packed + (strip * steps + step) * 1024) + lane;
+    const uint4* from = (const uint4*)(packed + strip + (size_t)step * 1024) + lane;
     uint4 q[4];
     float scale[4];
 #pragma unroll
@@ -301,7 +301,7 @@ extern "C" {
 size_t bigmac_mx_scale_bytes(int64_t cols) { return cols < 1 || cols > MAX_COLS ? 0 : mx_scale_bytes(cols); }
 
 size_t bigmac_mx_packed_bytes(int32_t groups, int32_t n_in, int32_t n_out) {
-  return check_weights(groups, n_in, n_out) == BIGMAC_OK ? mx_packed(groups, n_in, n_out).bytes : 0;
+  return check_weights(groups, n_in, n_out) == BIGMAC_OK ? mx_packed_bytes(groups, n_in, n_out) : 0;
 }
 
 int bigmac_mx_quantize(int64_t rows, int64_t cols, int32_t dtype, const void* src, void* codes, void* scales, void* stream) {
@@ -328,11 +328,10 @@ int bigmac_mx_pack(int32_t groups, int32_t n_in, int32_t n_out, int32_t dtype, c
   const int rc = check_weights(groups, n_in, n_out);
   if (rc) return rc;
   if ((dtype != BIGMAC_F32 && dtype != BIGMAC_BF16) || !w || !packed || !aligned({w, packed})) return BIGMAC_ERR_INVALID_ARG;
-  const size_t scales_at = mx_packed(groups, n_in, n_out).scales_at;
   const unsigned blocks = pack_blocks(groups, n_in, n_out);
   hipStream_t s = (hipStream_t)stream;
-  if (dtype == BIGMAC_BF16) mx_pack_kernel<bf16_t><<<blocks, 256, 0, s>>>((const bf16_t*)w, (uint8_t*)packed, scales_at, groups, n_in, n_out);
-  else mx_pack_kernel<float><<<blocks, 256, 0, s>>>((const float*)w, (uint8_t*)packed, scales_at, groups, n_in, n_out);
+  if (dtype == BIGMAC_BF16) mx_pack_kernel<bf16_t><<<blocks, 256, 0, s>>>((const bf16_t*)w, (uint8_t*)packed, groups, n_in, n_out);
+  else mx_pack_kernel<float><<<blocks, 256, 0, s>>>((const float*)w, (uint8_t*)packed, groups, n_in, n_out);
   BIGMAC_CHECK_LAUNCH();
   return BIGMAC_OK;
 }
@@ -341,11 +340,10 @@ int bigmac_mx_unpack(int32_t groups, int32_t n_in, int32_t n_out, const void* pa
   const int rc = check_weights(groups, n_in, n_out);
   if (rc) return rc;
   if ((dtype != BIGMAC_F32 && dtype != BIGMAC_BF16) || !w || !packed || !aligned({w, packed})) return BIGMAC_ERR_INVALID_ARG;
-  const size_t scales_at = mx_packed(groups, n_in, n_out).scales_at;
   const unsigned blocks = pack_blocks(groups, n_in, n_out);
   hipStream_t s = (hipStream_t)stream;
-  if (dtype == BIGMAC_BF16) mx_unpack_kernel<bf16_t><<<blocks, 256, 0, s>>>((const uint8_t*)packed, scales_at, (bf16_t*)w, groups, n_in, n_out);
-  else mx_unpack_kernel<float><<<blocks, 256, 0, s>>>((const uint8_t*)packed, scales_at, (float*)w, groups, n_in, n_out);
+  if (dtype == BIGMAC_BF16) mx_unpack_kernel<bf16_t><<<blocks, 256, 0, s>>>((const uint8_t*)packed, (bf16_t*)w, groups, n_in, n_out);
+  else mx_unpack_kernel<float><<<blocks, 256, 0, s>>>((const uint8_t*)packed, (float*)w, groups, n_in, n_out);
   BIGMAC_CHECK_LAUNCH();
   return BIGMAC_OK;
 }
@@ -364,12 +362,13 @@ int bigmac_mx_product(const bigmac_mx_dims* D, const void* codes, const void* sc
   p.out = out;
   p.rows = D->rows; p.groups = D->groups; p.n_in = D->n_in; p.n_out = D->n_out;
   p.epilogue = D->out_dtype == BIGMAC_F32 ? MX_STORE_F32 : MX_STORE_BF16;
+  p.tile_rows = mx_tile_rows(D->rows, D->groups, D->n_out);
   if (offsets) {
     if (!ws || !aligned({ws})) return BIGMAC_ERR_INVALID_ARG;
     if (ws_bytes < mx_map_bytes(D->rows, D->groups)) return BIGMAC_ERR_WORKSPACE;
     p.offsets = offsets;
     p.tile_map = (const int*)ws;
-    mx_map_kernel<<<1, 256, 0, s>>>(MxMapJob{offsets, (int*)ws, D->groups, mx_tile_rows(D->rows, D->groups)});
+    mx_map_kernel<<<1, 256, 0, s>>>(MxMapJob{offsets, (int*)ws, D->groups, p.tile_rows});
     BIGMAC_CHECK_LAUNCH();
   }
   return launch_mx_product(p, s);
@@ -389,12 +388,12 @@ int bigmac_mx_grouped_ffn(const bigmac_dims* D, const void* x_perm, const int32_
   hipStream_t s = (hipStream_t)stream;
   const int rows = (int)((long)D->T * D->k);
   uint8_t* base = (uint8_t*)ws;
-  const MxMapJob map{expert_offsets, (int*)(base + plan.map), D->N, mx_tile_rows(rows, D->N)};
+  const MxMapJob map{expert_offsets, (int*)(base + plan.map), D->N, mx_tile_rows(rows, D->N, std::min(W.win, W.hid))};
   rc = launch_mx_quantize(rows, W.win, BIGMAC_BF16, x_perm, base + plan.x_codes, base + plan.x_scales, s, &map);
   if (rc) return rc;
   MxProduct p{};
   p.codes = base + plan.x_codes; p.scales = base + plan.x_scales; p.packed = (const uint8_t*)w1; p.bias = (const bf16_t*)b1;
-  p.offsets = expert_offsets; p.tile_map = map.map;
+  p.offsets = expert_offsets; p.tile_map = map.map; p.tile_rows = map.tile_rows;
   p.out = base + plan.h_codes; p.out_scales = base + plan.h_scales;
   p.rows = rows; p.groups = D->N; p.n_in = W.win; p.n_out = W.hid; p.epilogue = MX_GELU_CODES;
   rc = launch_mx_product(p, s);

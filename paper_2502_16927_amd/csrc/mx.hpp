@@ -14,15 +14,12 @@ inline size_t mx_scale_bytes(long cols) { return (size_t)((cols + MX_CHUNK - 1) 
 __device__ __forceinline__ unsigned mx_scale_at(unsigned block) { return (block & ~7u) + (block & 1) * 4 + ((block & 7) >> 1); }
 
 // Weights: 32 output columns x 64 inputs are the 1 KB that a wavefront feeds to one matrix instruction, lane l's 16 bytes (column l % 32,
-// inputs 32 (l / 32) .. + 31) one after another: [group][n_out / 32][n_in / 64][64 lanes][16].  Behind all codes the scales,
-// [group][n_out / 32][n_in / 256, rounded up][64 lanes][4]: byte j of a lane for its j-th instruction of the 256 inputs.
-struct MxPacked {
-  size_t scales_at, bytes;
-};
-inline MxPacked mx_packed(long groups, long n_in, long n_out) {
-  const size_t codes = (size_t)groups * n_in * n_out / 2;
-  return {codes, align_up(codes + (size_t)groups * (n_out / 32) * ((n_in + MX_CHUNK - 1) / MX_CHUNK) * 256)};
-}
+// inputs 32 (l / 32) .. + 31) one after another.  A strip of 32 columns: [n_in / 64][64 lanes][16] codes, behind them its scales,
+// [n_in / 256, rounded up][64 lanes][4]: byte j of a lane for its j-th instruction of the 256 inputs.  [groups][n_out / 32] strips.
+// (With the scales behind all codes the strips lie a power of two apart where n_in is one, and wavefronts that read the same inputs of
+// different strips meet on a few of the L2's channels.)
+inline __host__ __device__ size_t mx_strip_bytes(long n_in) { return (size_t)(n_in / MX_STEP) * 1024 + (size_t)((n_in + MX_CHUNK - 1) / MX_CHUNK) * 256; }
+inline size_t mx_packed_bytes(long groups, long n_in, long n_out) { return (size_t)groups * (n_out / 32) * mx_strip_bytes(n_in); }
 
 // Scale byte of a block from the largest magnitude's bits: floor(log2) - 2, not under 2^-127; 255 where the block holds an infinity or NaN.
 __device__ __forceinline__ unsigned mx_scale_byte(unsigned top_bits) {
@@ -64,8 +61,9 @@ struct MxProduct {
   void* out;                       // [rows][n_out] bf16 or fp32, or codes
   uint8_t* out_scales;             // MX_GELU_CODES: of the rows of codes
   int rows, groups, n_in, n_out, epilogue;
+  int tile_rows;                   // from mx_tile_rows, as the tile map's
 };
-int mx_tile_rows(int rows, int groups);
+int mx_tile_rows(int rows, int groups, int n_out);
 int launch_mx_product(const MxProduct& p, hipStream_t s);
 // The row tiles of a ragged product: map[0] = how many, then from map[2] on (group, first row) of each, groups in order
 struct MxMapJob {

@@ -4,6 +4,7 @@
 //
 // The results are worked out transposed (the weights are the instruction's first operand), so a lane holds 16 columns of one row:
 // a block of 32 hidden columns lies in lanes l and l + 32, which is what the GELU epilogue needs to make 4-bit rows of it.
+#include <algorithm>
 #include <type_traits>
 
 #include "mx.hpp"
@@ -14,6 +15,7 @@ namespace bigmac {
 namespace {
 
 typedef int i32x8_t __attribute__((ext_vector_type(8)));
+
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t scalar_buffer(size_t at, size_t bytes) {
   const unsigned lo = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)at), hi = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(at >> 32));
@@ -66,17 +68,17 @@ struct MxTile {
   int group, m0, m_rows, strip0;   // strip0: first 32 columns of the workgroup
   bool valid;
 };
-template <int BM, int STRIPS>
-__device__ __forceinline__ MxTile mx_tile(const MxProduct& p) {
+// Tiles of BM rows x `parts` parts of the columns.  Consecutive workgroups go to the 8 XCDs in turn: each XCD gets a run of consecutive tiles,
+// column parts fastest.  strip0: which part.
+template <int BM>
+__device__ __forceinline__ MxTile mx_part(const MxProduct& p, int parts) {
   MxTile t;
-  const int strips = p.n_out / 32, gx = (strips + STRIPS - 1) / STRIPS;
   const int tiles = p.offsets ? table_at(p.tile_map, 0) : (p.rows + BM - 1) / BM;
-  // consecutive workgroups go to the 8 XCDs in turn: each XCD gets a run of consecutive tiles, column tiles fastest
-  const unsigned total = (unsigned)tiles * (unsigned)gx, per_xcd = (total + 7) / 8, slot = blockIdx.x >> 3, id = (blockIdx.x & 7) * per_xcd + slot;
+  const unsigned total = (unsigned)tiles * (unsigned)parts, per_xcd = (total + 7) / 8, slot = blockIdx.x >> 3, id = (blockIdx.x & 7) * per_xcd + slot;
   t.valid = slot < per_xcd && id < total;
   if (!t.valid) return t;
-  const int tile = (int)(id / (unsigned)gx);
-  t.strip0 = (int)(id % (unsigned)gx) * STRIPS;
+  const int tile = (int)(id / (unsigned)parts);
+  t.strip0 = (int)(id % (unsigned)parts);
   int m_end = p.rows;
   t.group = 0;
   t.m0 = tile * BM;
@@ -86,6 +88,13 @@ __device__ __forceinline__ MxTile mx_tile(const MxProduct& p) {
     m_end = table_at(p.offsets, t.group + 1);
   }
   t.m_rows = min(m_end - t.m0, BM);
+  return t;
+}
+// ... the parts STRIPS x 32 columns each; strip0: the first 32 columns
+template <int BM, int STRIPS>
+__device__ __forceinline__ MxTile mx_tile(const MxProduct& p) {
+  MxTile t = mx_part<BM>(p, (p.n_out / 32 + STRIPS - 1) / STRIPS);
+  t.strip0 *= STRIPS;
   return t;
 }
 
@@ -134,10 +143,10 @@ __device__ __forceinline__ void mx_store(const MxProduct& p, const f32x16_t (&ac
     strip_out(strip, p, row0, rows, (size_t)(col0 + 32 * j) * 4, (size_t)p.n_out * 4, lane);
   }
 }
-// GELU and 4 bits: 32 rows x 64 columns of a wavefront into the workgroup's [rows][256 columns] of codes (128 bytes a row) and [rows][8] of scales
+// GELU and 4 bits of 32 rows x 64 columns: a block of a row per lane, the first 32 columns in the lower lanes; bytes: both blocks' scales
 template <int NS>
-__device__ __forceinline__ void mx_gelu_codes(const f32x16_t (&acc)[NS], const float (&bias)[NS][16], bool biased, char* codes, uint8_t* scales, int row0, int wave, int lane) {
-  static_assert(NS == 2, "a wavefront's 64 columns are two blocks");
+__device__ __forceinline__ uint4 mx_gelu_blocks(const f32x16_t (&acc)[NS], const float (&bias)[NS][16], bool biased, unsigned (&bytes)[NS]) {
+  static_assert(NS == 2, "a lane for each block");
   uint2 half_block[NS];   // lower lane: columns 0 .. 15 of a block, upper lane: 16 .. 31
 #pragma unroll
   for (int j = 0; j < NS; ++j) {
@@ -152,16 +161,31 @@ __device__ __forceinline__ void mx_gelu_codes(const f32x16_t (&acc)[NS], const f
     const unsigned mine = __float_as_uint(top_of(f));
     const auto both = __builtin_amdgcn_permlane32_swap(mine, mine, false, false);
     // the smallest scale here is 2^-126: values of a block under 2^-124 that 2^-127 would hold better
-    const unsigned byte = max(mx_scale_byte(max(both[0], both[1]) & 0x7FFFFFFFu), 1u);   // (a NaN is the largest, with its sign or without)
+    bytes[j] = max(mx_scale_byte(max(both[0], both[1]) & 0x7FFFFFFFu), 1u);   // (a NaN is the largest, with its sign or without)
     // halfword q: this lane's four columns of quad q; lower lane: the lower and the upper lane's of quads 0 and 1, upper lane: of quads 2 and 3
-    const auto r = __builtin_amdgcn_permlane32_swap(mx_codes8_scaled(f, byte), mx_codes8_scaled(f + 8, byte), false, false);
+    const auto r = __builtin_amdgcn_permlane32_swap(mx_codes8_scaled(f, bytes[j]), mx_codes8_scaled(f + 8, bytes[j]), false, false);
     half_block[j] = make_uint2((r[0] & 0xFFFFu) | (r[1] << 16), (r[0] >> 16) | (r[1] & 0xFFFF0000u));
-    if (lane < 32) scales[(row0 + lane) * 8 + j * 4 + wave] = (uint8_t)byte;
   }
-  // whole blocks: the first in the lower lane, the second in the upper
   const auto x = __builtin_amdgcn_permlane32_swap(half_block[0].x, half_block[1].x, false, false);
   const auto y = __builtin_amdgcn_permlane32_swap(half_block[0].y, half_block[1].y, false, false);
-  *(uint4*)(codes + piece_place(row0 + (lane & 31), wave * 2 + (lane >> 5))) = make_uint4(x[0], y[0], x[1], y[1]);
+  return make_uint4(x[0], y[0], x[1], y[1]);
+}
+// biases of the columns a lane holds of the 32 NS from `strip` on (bias NULL: zeros)
+template <int NS>
+__device__ __forceinline__ void mx_bias(const MxProduct& p, const MxTile& t, int strip, float (&bias)[NS][16], int lane) {
+#pragma unroll
+  for (int j = 0; j < NS; ++j)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) bias[j][v] = 0.0f;
+  if (!p.bias) return;
+#pragma unroll
+  for (int j = 0; j < NS; ++j)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const uint2 b = *(const uint2*)(p.bias + (size_t)t.group * p.n_out + (strip + j) * 32 + 8 * q + 4 * (lane >> 5));
+      bias[j][4 * q] = __uint_as_float(b.x << 16); bias[j][4 * q + 1] = __uint_as_float(b.x & 0xFFFF0000u);
+      bias[j][4 * q + 2] = __uint_as_float(b.y << 16); bias[j][4 * q + 3] = __uint_as_float(b.y & 0xFFFF0000u);
+    }
 }
 
 // MT x 32 rows, 4 wavefronts side by side with NS x 32 columns each.
@@ -170,31 +194,26 @@ __device__ __forceinline__ void mx_gelu_codes(const f32x16_t (&acc)[NS], const f
 // Rows go straight to the LDS in chunks of 256 inputs, three stages: while chunk c is multiplied, chunk c + 1 has landed or is about
 // to and chunk c + 2 is requested.  A chunk's step: the eight (MT NS) instructions of 64 inputs, between them the LDS reads of the next
 // step's fragments, behind them the next chunk's weights of the same step, into the registers that have just been read.
+constexpr int MX_STAGES = 3;
+constexpr unsigned mx_stage_bytes(int mt) { return mt * 4096 + 1024; }   // codes; 256 dwords of scales (past the tile's rows: zeros)
 template <int MT, int NS, int EPI>
-__global__ __launch_bounds__(256, MT * NS == 8 ? 2 : 3) void mx_product_kernel(MxProduct p) {
-  constexpr int BM = MT * 32, STRIPS = 4 * NS, STAGES = 3;
-  constexpr unsigned CODES = BM * 128, STAGE = CODES + 1024;     // bytes; 256 dwords of scales (past row BM: zeros)
-  __shared__ uint4 ring[STAGES * STAGE / 16];
-  constexpr int OUT = EPI == MX_GELU_CODES ? BM * 128 : 4 * 4096;
-  __shared__ uint4 staging[OUT / 16];
-  __shared__ __align__(16) uint8_t out_scales[EPI == MX_GELU_CODES ? BM * 8 : 8];
+__device__ __forceinline__ void mx_tile_product(const MxProduct& p, const MxTile& t, uint4* ring, uint4* staging, uint8_t* out_scales) {
+  constexpr int STAGES = MX_STAGES;
+  constexpr unsigned CODES = MT * 4096, STAGE = mx_stage_bytes(MT);
   const unsigned ring_at = lds_address(ring);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const MxTile t = mx_tile<BM, STRIPS>(p);
-  if (!t.valid) return;
   const int strips = p.n_out / 32, strip0 = t.strip0 + wave * NS;
   const int steps = p.n_in / MX_STEP, chunks = (steps + 3) / 4;
   const unsigned row_bytes = (unsigned)p.n_in / 2, scale_bytes = (unsigned)chunks * 8;
   const auto ba = scalar_buffer((size_t)p.codes + (size_t)t.m0 * row_bytes, (size_t)t.m_rows * row_bytes);
   const auto bs = scalar_buffer((size_t)p.scales + (size_t)t.m0 * scale_bytes, (size_t)t.m_rows * scale_bytes);
-  const size_t scales_at = (size_t)p.groups * p.n_in * p.n_out / 2;
-  __amdgpu_buffer_rsrc_t bw[NS], bws[NS];
+  const unsigned strip_bytes = (unsigned)mx_strip_bytes(p.n_in), scales_at = (unsigned)steps * 1024u;   // of a strip of the weights
+  __amdgpu_buffer_rsrc_t bw[NS];
 #pragma unroll
   for (int j = 0; j < NS; ++j) {
     const bool there = strip0 + j < strips;   // past the last column: empty ranges, zeros
     const size_t strip = (size_t)t.group * strips + (there ? strip0 + j : 0);
-    bw[j] = scalar_buffer((size_t)p.packed + strip * steps * 1024, there ? (size_t)steps * 1024 : 0);
-    bws[j] = scalar_buffer((size_t)p.packed + scales_at + strip * chunks * 256, there ? (size_t)chunks * 256 : 0);
+    bw[j] = scalar_buffer((size_t)p.packed + strip * strip_bytes, there ? strip_bytes : 0);
   }
 
   // LDS place q (16 bytes) of a stage: row q / 8, piece (q % 8) ^ (row / 2 % 8) of it: 16 consecutive rows at one piece lie on all banks
@@ -222,11 +241,11 @@ __global__ __launch_bounds__(256, MT * NS == 8 ? 2 : 3) void mx_product_kernel(M
   auto load_w = [&](int chunk, auto ks) {
     constexpr int J = decltype(ks)::value;
 #pragma unroll
-    for (int j = 0; j < NS; ++j) w[j][J] = __builtin_amdgcn_raw_buffer_load_b128(bw[j], (unsigned)(chunk * 4 + J) * 1024u + w_off, 0, 0);
+    for (int j = 0; j < NS; ++j) w[j][J] = __builtin_amdgcn_raw_buffer_load_b128(bw[j], chunk * 4 + J < steps ? (unsigned)(chunk * 4 + J) * 1024u + w_off : 0x80000000u, 0, 0);
   };
   auto load_ws = [&](int chunk) {
 #pragma unroll
-    for (int j = 0; j < NS; ++j) ws_next[j] = __builtin_amdgcn_raw_buffer_load_b32(bws[j], (unsigned)chunk * 256u + ws_off, 0, 0);
+    for (int j = 0; j < NS; ++j) ws_next[j] = __builtin_amdgcn_raw_buffer_load_b32(bw[j], scales_at + (unsigned)chunk * 256u + ws_off, 0, 0);
   };
   const unsigned fa_at = ring_at + (unsigned)(lane & 31) * 128u + (((unsigned)lane >> 5) ^ (((unsigned)lane >> 1) & 7)) * 16u;
   const unsigned as_at = ring_at + CODES + (unsigned)(lane & 31) * 8u + ((unsigned)lane >> 5) * 4u;
@@ -331,24 +350,16 @@ __global__ __launch_bounds__(256, MT * NS == 8 ? 2 : 3) void mx_product_kernel(M
 
   const bool there = strip0 < strips;       // (strips are whole pairs)
   float bias[NS][16];
-#pragma unroll
-  for (int j = 0; j < NS; ++j)
-#pragma unroll
-    for (int v = 0; v < 16; ++v) bias[j][v] = 0.0f;
-  if (p.bias && there)
-#pragma unroll
-    for (int j = 0; j < NS; ++j)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const uint2 b = *(const uint2*)(p.bias + (size_t)t.group * p.n_out + (strip0 + j) * 32 + 8 * q + 4 * (lane >> 5));
-        bias[j][4 * q] = __uint_as_float(b.x << 16); bias[j][4 * q + 1] = __uint_as_float(b.x & 0xFFFF0000u);
-        bias[j][4 * q + 2] = __uint_as_float(b.y << 16); bias[j][4 * q + 3] = __uint_as_float(b.y & 0xFFFF0000u);
-      }
+  mx_bias<NS>(p, t, there ? strip0 : t.strip0, bias, lane);
   if constexpr (EPI == MX_GELU_CODES) {
     if (there) {
 #pragma unroll
       for (int i = 0; i < MT; ++i)
-        if (i * 32 < t.m_rows) mx_gelu_codes<NS>(acc[i], bias, p.bias != nullptr, (char*)staging, out_scales, i * 32, wave, lane);
+        if (i * 32 < t.m_rows) {
+          unsigned bytes[NS];
+          *(uint4*)((char*)staging + piece_place(i * 32 + (lane & 31), wave * 2 + (lane >> 5))) = mx_gelu_blocks<NS>(acc[i], bias, p.bias != nullptr, bytes);
+          out_scales[(i * 32 + (lane & 31)) * 8 + (lane >> 5) * 4 + wave] = (uint8_t)(lane < 32 ? bytes[0] : bytes[1]);   // blocks 2 wave and 2 wave + 1: see mx.hpp
+        }
     }
     __syncthreads();
     const size_t row_out = (size_t)p.n_out / 2, scales_out = (size_t)((p.n_out + MX_CHUNK - 1) / MX_CHUNK) * 8;
@@ -371,33 +382,171 @@ __global__ __launch_bounds__(256, MT * NS == 8 ? 2 : 3) void mx_product_kernel(M
   }
 }
 
-template <int MT, int NS>
+template <int MT, int NS, int EPI>
+__global__ __launch_bounds__(256, MT == 4 ? 2 : 4) void mx_product_kernel(MxProduct p) {
+  constexpr int BM = MT * 32;
+  __shared__ uint4 ring[MX_STAGES * mx_stage_bytes(MT) / 16];
+  __shared__ uint4 staging[(EPI == MX_GELU_CODES ? BM * 128 : 4 * 4096) / 16];
+  __shared__ __align__(16) uint8_t out_scales[EPI == MX_GELU_CODES ? BM * 8 : 8];
+  const MxTile t = mx_tile<BM, 4 * NS>(p);
+  if (!t.valid) return;
+  if constexpr (MT == 4) {   // the last rows of a group
+    if (t.m_rows <= 32) return mx_tile_product<1, NS, EPI>(p, t, ring, staging, out_scales);
+    if (t.m_rows <= 64) return mx_tile_product<2, NS, EPI>(p, t, ring, staging, out_scales);
+    if (t.m_rows <= 96) return mx_tile_product<3, NS, EPI>(p, t, ring, staging, out_scales);
+  }
+  mx_tile_product<MT, NS, EPI>(p, t, ring, staging, out_scales);
+}
+
+// Few tiles, long rows: MT x 32 rows x 64 columns per workgroup, its four wavefronts each a quarter of the inputs, their sums joined in
+// the LDS in the wavefronts' order.  With as many workgroups as fill the chip at 64 columns a row tile's operands are re-read four
+// times as often as at 256, but nothing waits for a serial walk over all inputs.  Both operands go straight to registers, a chunk ahead; no
+// barrier before the join.
+template <int MT, int EPI>
+__global__ __launch_bounds__(256, 2) void mx_split_kernel(MxProduct p) {
+  constexpr int BM = MT * 32, NS = 2;
+  __shared__ float join[3][MT * NS * 16][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const MxTile t = mx_tile<BM, NS>(p);
+  if (!t.valid) return;
+  const int strips = p.n_out / 32, steps = p.n_in / MX_STEP, chunks = (steps + 3) / 4;
+  const unsigned row_bytes = (unsigned)p.n_in / 2, scale_bytes = (unsigned)chunks * 8;
+  const auto ba = scalar_buffer((size_t)p.codes + (size_t)t.m0 * row_bytes, (size_t)t.m_rows * row_bytes);
+  const auto bs = scalar_buffer((size_t)p.scales + (size_t)t.m0 * scale_bytes, (size_t)t.m_rows * scale_bytes);
+  const unsigned strip_bytes = (unsigned)mx_strip_bytes(p.n_in), scales_at = (unsigned)steps * 1024u;   // of a strip of the weights
+  __amdgpu_buffer_rsrc_t bw[NS];
+#pragma unroll
+  for (int j = 0; j < NS; ++j) {
+    const size_t strip = (size_t)t.group * strips + t.strip0 + j;
+    bw[j] = scalar_buffer((size_t)p.packed + strip * strip_bytes, strip_bytes);
+  }
+  const unsigned a_off = (unsigned)(lane & 31) * row_bytes + ((unsigned)lane >> 5) * 16u, s_off = (unsigned)(lane & 31) * scale_bytes + ((unsigned)lane >> 5) * 4u;
+  struct Chunk {
+    u32x4_t w[NS][4], a[MT][4];
+    unsigned ws[NS], as[MT];
+  };
+  // (past the last input: weights out of range, zeros; the rows' codes are another row's, their scales are cut off below)
+  auto load = [&](Chunk& c, int chunk) {
+#pragma unroll
+    for (int j = 0; j < NS; ++j) {
+      c.ws[j] = __builtin_amdgcn_raw_buffer_load_b32(bw[j], scales_at + (unsigned)chunk * 256u + lane * 4u, 0, 0);
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) c.w[j][ks] = __builtin_amdgcn_raw_buffer_load_b128(bw[j], chunk * 4 + ks < steps ? (unsigned)(chunk * 4 + ks) * 1024u + lane * 16u : 0x80000000u, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      c.as[i] = __builtin_amdgcn_raw_buffer_load_b32(bs, s_off + i * 32u * scale_bytes + (unsigned)chunk * 8u, 0, 0);
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) c.a[i][ks] = __builtin_amdgcn_raw_buffer_load_b128(ba, a_off + i * 32u * row_bytes + (unsigned)chunk * 128u + ks * 32u, 0, 0);
+    }
+  };
+  f32x16_t acc[MT][NS];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NS; ++j) acc[i][j] = f32x16_t{0};
+  const unsigned last_mask = steps & 3 ? (1u << (8 * (steps & 3))) - 1u : ~0u;   // (a scale byte of 255 there would make NaN of the weights' zeros)
+  auto multiply = [&](const Chunk& c, int chunk) {
+    static_for<0, MT * NS>([&](auto n) {
+      constexpr int i = decltype(n)::value / NS, j = decltype(n)::value % NS;
+      const unsigned as = chunk + 1 == chunks ? c.as[i] & last_mask : c.as[i];
+      static_for<0, 4>([&](auto ks) { acc[i][j] = mx_mfma<decltype(ks)::value>(c.w[j][decltype(ks)::value], c.ws[j], c.a[i][decltype(ks)::value], as, acc[i][j]); });
+    });
+  };
+  // this wavefront's chunks
+  const int first = chunks * wave / 4, last = chunks * (wave + 1) / 4;
+  Chunk one, two;
+  if (first < last) {
+    load(one, first);
+    int c = first;
+    for (; c + 1 < last; c += 2) {
+      load(two, c + 1);
+      multiply(one, c);
+      load(one, min(c + 2, last - 1));
+      multiply(two, c + 1);
+    }
+    if (c < last) multiply(one, c);
+  }
+  if (wave > 0)
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int j = 0; j < NS; ++j)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) join[wave - 1][(i * NS + j) * 16 + v][lane] = acc[i][j][v];
+  __syncthreads();
+  if (wave > 0) return;
+  float bias[NS][16];
+  mx_bias<NS>(p, t, t.strip0, bias, lane);
+  __shared__ uint4 staging[4096 / 16];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    if (i * 32 >= t.m_rows) break;
+#pragma unroll
+    for (int w = 0; w < 3; ++w)
+#pragma unroll
+      for (int j = 0; j < NS; ++j)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[i][j][v] += join[w][(i * NS + j) * 16 + v][lane];
+    if constexpr (EPI == MX_GELU_CODES) {
+      unsigned bytes[NS];
+      const uint4 block = mx_gelu_blocks<NS>(acc[i], bias, p.bias != nullptr, bytes);
+      const int row = i * 32 + (lane & 31);
+      if (row < t.m_rows) {
+        *(uint4*)((uint8_t*)p.out + (size_t)(t.m0 + row) * (p.n_out / 2) + (size_t)(t.strip0 + (lane >> 5)) * 16) = block;
+        p.out_scales[(size_t)(t.m0 + row) * ((p.n_out + MX_CHUNK - 1) / MX_CHUNK * 8) + mx_scale_at(t.strip0 + (lane >> 5))] = (uint8_t)(lane < 32 ? bytes[0] : bytes[1]);
+      }
+    } else {
+      mx_store<NS>(p, acc[i], bias, t.m0 + i * 32, t.m_rows - i * 32, t.strip0 * 32, (char*)staging, lane, std::integral_constant<int, EPI>{});
+    }
+  }
+}
+
+// upper bound of the row tiles
+long most_tiles(const MxProduct& p, int tile_rows) {
+  return p.offsets ? (long)p.rows / tile_rows + std::min(p.groups, p.rows) : ((long)p.rows + tile_rows - 1) / tile_rows;
+}
+template <int MT>
 int launch_of(const MxProduct& p, hipStream_t s) {
-  const long tiles = p.offsets ? (long)p.rows / (MT * 32) + p.groups : ((long)p.rows + MT * 32 - 1) / (MT * 32);
-  const long gx = (p.n_out / 32 + 4 * NS - 1) / (4 * NS);
-  const long blocks = (tiles * gx + 7) / 8 * 8;
+  const long gx = (p.n_out + 255) / 256, blocks = (most_tiles(p, MT * 32) * gx + 7) / 8 * 8;
   if (blocks > 0x3FFFFFFFl) return BIGMAC_ERR_TOO_LARGE;
   const dim3 grid((unsigned)blocks);
-  if (p.epilogue == MX_GELU_CODES) mx_product_kernel<MT, NS, MX_GELU_CODES><<<grid, 256, 0, s>>>(p);
-  else if (p.epilogue == MX_STORE_F32) mx_product_kernel<MT, NS, MX_STORE_F32><<<grid, 256, 0, s>>>(p);
-  else mx_product_kernel<MT, NS, MX_STORE_BF16><<<grid, 256, 0, s>>>(p);
+  if (p.epilogue == MX_GELU_CODES) mx_product_kernel<MT, 2, MX_GELU_CODES><<<grid, 256, 0, s>>>(p);
+  else if (p.epilogue == MX_STORE_F32) mx_product_kernel<MT, 2, MX_STORE_F32><<<grid, 256, 0, s>>>(p);
+  else mx_product_kernel<MT, 2, MX_STORE_BF16><<<grid, 256, 0, s>>>(p);
+  BIGMAC_CHECK_LAUNCH();
+  return BIGMAC_OK;
+}
+int launch_split(const MxProduct& p, hipStream_t s) {
+  const long blocks = (most_tiles(p, 32) * (p.n_out / 64) + 7) / 8 * 8;
+  if (blocks > 0x3FFFFFFFl) return BIGMAC_ERR_TOO_LARGE;
+  const dim3 grid((unsigned)blocks);
+  if (p.epilogue == MX_GELU_CODES) mx_split_kernel<1, MX_GELU_CODES><<<grid, 256, 0, s>>>(p);
+  else if (p.epilogue == MX_STORE_F32) mx_split_kernel<1, MX_STORE_F32><<<grid, 256, 0, s>>>(p);
+  else mx_split_kernel<1, MX_STORE_BF16><<<grid, 256, 0, s>>>(p);
   BIGMAC_CHECK_LAUNCH();
   return BIGMAC_OK;
 }
 
 }  // namespace
 
-int mx_tile_rows(int rows, int groups) {
-  const int even = rows / groups;
-  return even > 64 ? 128 : even > 32 ? 64 : 32;
+// Rows per tile.  A tile of 128 rows reads its weights once for all of them, and one with fewer rows leaves out whole sub-tiles of 32; 32-row
+// tiles fill more of the chip.  Where the 128-row tiles (rows spread evenly over the groups) would be fewer than 128, half of the CUs: 32.  Measured
+// on both sides, us with 128 and 32 rows: 1024 dense rows 4096 -> 1024 (32 tiles) 15.6, 10.2; 2048 (64) 16.2, 11.5; 4096 (128) 17.2, 19.0;
+// 2048 rows 1024 -> 4096 (256) 10.8, 12.9; 8 groups of 250 rows 4096 -> 1024 (64) 19.2, 14.7; 1024 -> 4096 of 8 x 125 (128) 11.4, 11.5.
+// n_out: of the narrowest product that walks the tiles.
+long even_tiles(long rows, long groups, int tile_rows) {
+  const long busy = std::min(rows, groups), each = (rows + busy - 1) / busy;
+  return busy * ((each + tile_rows - 1) / tile_rows);
 }
+int mx_tile_rows(int rows, int groups, int n_out) { return even_tiles(rows, groups, 128) * ((n_out + 255) / 256) < 128 ? 32 : 128; }
 
 int launch_mx_product(const MxProduct& p, hipStream_t s) {
-  switch (mx_tile_rows(p.rows, p.groups)) {
-    case 32: return launch_of<1, 2>(p, s);
-    case 64: return launch_of<2, 2>(p, s);
-    default: return launch_of<4, 2>(p, s);
-  }
+  if (p.tile_rows == 128) return launch_of<4>(p, s);
+  // A quarter of the inputs per wavefront, for few tiles and a long walk: us without and with at 4096 inputs, 1024 columns: 1 row 8.4, 6.1;
+  // 500 (64 tiles of 256 columns) 10.0, 8.3; 8 groups of 32 (32) 12.8, 10.9; 16 of 16 (64) 13.2, 12.3; 8 of 125 (128) 13.1, 15.6; at 1024 inputs within 0.4
+  if (p.n_in >= 2048 && even_tiles(p.rows, p.groups, 32) * ((p.n_out + 255) / 256) <= 64) return launch_split(p, s);
+  return launch_of<1>(p, s);
 }
 
 }  // namespace bigmac

@@ -164,6 +164,26 @@ def test_dense_products(rows):
     check_product([rows], 576, 448, dense=True, bias=rows % 2 == 0, out="bf16" if rows > 64 else "f32")
 
 
+# groups enough that the tiles have 128 rows; row counts around every sub-tile's edge
+EDGES = [0, 1, 31, 32, 33, 64, 65, 96, 97, 127, 128, 129, 200, 5, 0, 160]
+
+
+@pytest.mark.parametrize("n_in,n_out", [(64, 64), (320, 192), (1088, 64), (512, 320)])
+def test_tiles_of_128_rows(n_in, n_out):
+    counts = EDGES * 8
+    print(f"products of {sum(counts)} rows in {len(counts)} groups, {n_in} -> {n_out}", flush=True)
+    check_product(counts, n_in, n_out, seed=n_in)
+    check_product(counts, n_in, n_out, out="bf16", bias=True, spare=70, seed=n_in + 1)
+
+
+def test_one_row_and_few_rows_over_many_inputs():
+    """A quarter of the inputs per wavefront: inputs that end inside a chunk, fewer chunks for one wavefront than for another."""
+    for n_in in (2048, 2112, 2304, 4160):
+        for counts in ([1], [33], [3, 0, 40]):
+            check_product(counts, n_in, 128, out="f32", bias=True, seed=n_in)
+            check_product(counts, n_in, 64, out="bf16", dense=len(counts) == 1, seed=n_in)
+
+
 def test_many_groups():
     rng = np.random.default_rng(3)
     check_product(list(rng.integers(0, 5, 700)), 64, 64)
@@ -258,7 +278,10 @@ class Ffn:
     (40, 4, 4, 320, 640, [70, 64, 20, 6]),
     (200, 2, 3, 256, 576, [129, 0, 271]),
     (64, 2, 2, 1024, 128, [128, 0]),
-], ids=str)
+    (20, 1, 2, 2112, 64, [7, 13]),
+    (12, 1, 2, 128, 2176, [0, 12]),
+    (sum(EDGES) * 4, 2, 128, 192, 320, EDGES * 8),
+], ids=lambda v: str(v)[:40])
 @pytest.mark.parametrize("bias", [False, True])
 def test_experts(T, k, N, r, h, counts, bias):
     print(f"experts T {T} k {k} N {N} r {r} h {h} {counts}", flush=True)
