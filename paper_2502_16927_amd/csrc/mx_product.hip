@@ -16,7 +16,6 @@ namespace {
 
 typedef int i32x8_t __attribute__((ext_vector_type(8)));
 
-
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t scalar_buffer(size_t at, size_t bytes) {
   const unsigned lo = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)at), hi = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(at >> 32));
   return __builtin_amdgcn_make_buffer_rsrc((void*)(((size_t)hi << 32) | lo), 0, __builtin_amdgcn_readfirstlane((int)bytes), 0x00020000);
@@ -266,19 +265,28 @@ __device__ __forceinline__ void mx_tile_product(const MxProduct& p, const MxTile
     acc[i][j] = mx_mfma<J>(w[j][J], ws[j], fa[J & 1][i], as[i], acc[i][j]);
     __builtin_amdgcn_sched_barrier(0);
   };
-  auto arrived = [&](auto ks) {   // the fragments of a step, and at a chunk's first step its scales
+  // The fragments of a step.  A chunk's first ones and its scales are waited for at the end of the chunk in front of it: registers that an LDS
+  // read still under way will write must not be there where the loop closes, because the compiler, which knows nothing of the read,
+  // copies values between registers there.
+  auto arrived = [&](auto ks) {
     constexpr int J = decltype(ks)::value;
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-#pragma unroll
-    for (int i = 0; i < MT; ++i) hold(fa[J & 1][i]);
     if constexpr (J == 0) {
 #pragma unroll
-      for (int i = 0; i < MT; ++i) {
-        hold(as_next[i]);
-        as[i] = as_next[i];
-      }
+      for (int i = 0; i < MT; ++i) as[i] = as_next[i];
 #pragma unroll
       for (int j = 0; j < NS; ++j) ws[j] = ws_next[j];
+    } else {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+      for (int i = 0; i < MT; ++i) hold(fa[J & 1][i]);
+    }
+  };
+  auto first_arrived = [&]() {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      hold(fa[0][i]);
+      hold(as_next[i]);
     }
   };
   // one step of 64 inputs; meanwhile the next step's fragments are read, behind step 3 the next chunk's first
@@ -304,6 +312,7 @@ __device__ __forceinline__ void mx_tile_product(const MxProduct& p, const MxTile
     load_w(chunk + 1, ks);
     if constexpr (J == 0) load_ws(chunk + 1);
     asm volatile("" ::: "memory");
+    if constexpr (J == 3) first_arrived();
   };
   constexpr std::integral_constant<int, 0> I0{};
   constexpr std::integral_constant<int, 1> I1{};
@@ -322,6 +331,7 @@ __device__ __forceinline__ void mx_tile_product(const MxProduct& p, const MxTile
   asm volatile("" ::: "memory");
   read_scales(0);
   static_for<0, MT>([&](auto n) { read_a(n, I0, 0); });
+  first_arrived();
   const int whole = steps / 4;              // chunks of four steps
   unsigned stage = 0;
 #pragma clang loop unroll(disable)
@@ -334,7 +344,7 @@ __device__ __forceinline__ void mx_tile_product(const MxProduct& p, const MxTile
     step(I3, stage, next, c);
     stage = next;
   }
-  // one to three steps more; the fragments of the first are on their way (of a chunk that is not there: zeros or old ones, not used)
+  // one to three steps more; the fragments of the first are there (of a chunk that is not: zeros or old ones, not used)
   const int left = steps - whole * 4;
   arrived(I0);
   if (left > 0) {
@@ -348,6 +358,7 @@ __device__ __forceinline__ void mx_tile_product(const MxProduct& p, const MxTile
     if (left > 2) one(I2);
   }
 
+  BIGMAC_WAIT_VMCNT(0);                     // what is on its way to the LDS past the last chunk (zeros) arrives before the workgroup may end
   const bool there = strip0 < strips;       // (strips are whole pairs)
   float bias[NS][16];
   mx_bias<NS>(p, t, there ? strip0 : t.strip0, bias, lane);
