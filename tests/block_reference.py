@@ -85,3 +85,33 @@ def quantise(v):
 def gelu(v):
     from scipy.special import erfc
     return 0.5 * v * erfc(-v / np.sqrt(2.0))
+
+
+def ffn(x, counts, w1, w2, b1=None, b2=None):
+    """The experts' FFN on 4-bit rows and held weights: (output, how far a bf16 result of the library may be off) per row.
+
+    A product of n inputs adds 64 + n / 64 times in fp32, each off by at most a step of the partial sum (2 u), and once for the bias.  Where a hidden value
+    lies within its own error of a border between two held values it may fall on either side: the output may be off by that step times the weight."""
+    outs, limits, at = [], [], 0
+    xq = quantise(x)[2]
+    for e, n in enumerate(counts):
+        a = xq[at:at + n]
+        pre, size = a @ w1[e], np.abs(a) @ np.abs(w1[e])
+        if b1 is not None:
+            pre, size = pre + b1[e], size + np.abs(b1[e])
+        h = gelu(pre)
+        # |gelu'| < 1.13; the library's GELU: a polynomial within 6.8e-7 of gelu (of |a| times it below 1), its exponential within a step, 1.2e-7
+        # of at most half of |a|
+        off = 1.13 * 2 * (65 + a.shape[1] / 64) * U32 * size + 8e-7 + 4 * U32 * np.abs(h)
+        q = quantise(h)[2]
+        moved = np.zeros_like(q)
+        for direction in (1.0, -1.0):                                # all magnitudes a little larger, a little smaller: also across a scale's border
+            there = quantise(np.where(h < 0, -1.0, 1.0) * np.maximum(np.abs(h) + direction * off, 0.0))[2]
+            moved = np.maximum(moved, np.abs(there - q))
+        want, osize = q @ w2[e], np.abs(q) @ np.abs(w2[e])
+        if b2 is not None:
+            want, osize = want + b2[e], osize + np.abs(b2[e])
+        outs.append(want)
+        limits.append(2 * (65 + h.shape[1] / 64) * U32 * osize + HALF_STEP["bf16"] * np.abs(want) * (1 + 2.0 ** -10) + (1 + HALF_STEP["bf16"]) * (moved @ np.abs(w2[e])))
+        at += n
+    return np.concatenate(outs), np.concatenate(limits)

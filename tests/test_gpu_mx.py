@@ -218,33 +218,6 @@ def test_a_row_that_is_not_finite_stays_alone():
 
 # ------------------------------------------------------------------ the experts' FFN
 
-def ffn_reference(x, counts, w1, w2, b1, b2):
-    """(output, tolerance) per row: see the head of this file."""
-    outs, limits, at = [], [], 0
-    xq = R.quantise(x)[2]
-    for e, n in enumerate(counts):
-        a = xq[at:at + n]
-        pre, size = a @ w1[e], np.abs(a) @ np.abs(w1[e])
-        if b1 is not None:
-            pre, size = pre + b1[e], size + np.abs(b1[e])
-        h = R.gelu(pre)
-        # |gelu'| < 1.13; the library's GELU: a polynomial within 6.8e-7 of gelu (of |a| times it below 1), its exponential within a step, 1.2e-7
-        # of at most half of |a|
-        off = 1.13 * 2 * (65 + a.shape[1] / 64) * R.U32 * size + 8e-7 + 4 * R.U32 * np.abs(h)
-        q = R.quantise(h)[2]
-        moved = np.zeros_like(q)
-        for direction in (1.0, -1.0):                                # all magnitudes a little larger, a little smaller: also across a scale's border
-            there = R.quantise(np.where(h < 0, -1.0, 1.0) * np.maximum(np.abs(h) + direction * off, 0.0))[2]
-            moved = np.maximum(moved, np.abs(there - q))
-        want, osize = q @ w2[e], np.abs(q) @ np.abs(w2[e])
-        if b2 is not None:
-            want, osize = want + b2[e], osize + np.abs(b2[e])
-        outs.append(want)
-        limits.append(2 * (65 + h.shape[1] / 64) * R.U32 * osize + R.HALF_STEP["bf16"] * np.abs(want) * (1 + 2.0 ** -10) + (1 + R.HALF_STEP["bf16"]) * (moved @ np.abs(w2[e])))
-        at += n
-    return np.concatenate(outs), np.concatenate(limits)
-
-
 class Ffn:
     def __init__(self, T, k, N, r, h, counts, bias, order=B.ORDER_DCCA, seed=0):
         g = torch.Generator(device=DEV).manual_seed(seed)
@@ -263,7 +236,7 @@ class Ffn:
 
     def check(self):
         rows = sum(self.counts)
-        want, limit = ffn_reference(up(self.x)[:rows], self.counts, self.h1, self.h2, None if self.b1 is None else up(self.b1), None if self.b2 is None else up(self.b2))
+        want, limit = R.ffn(up(self.x)[:rows], self.counts, self.h1, self.h2, None if self.b1 is None else up(self.b1), None if self.b2 is None else up(self.b2))
         off = np.abs(up(self.out)[:rows] - want)
         assert (off <= limit).all(), f"{int((off > limit).sum())} of {off.size} off, worst {np.nanmax(off / limit)} of the limit"
         assert (self.out[rows:] == 7.0).all(), "rows behind the last expert"
