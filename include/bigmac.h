@@ -358,7 +358,9 @@ int bigmac_norm_backward(const bigmac_norm_dims *dims, const bigmac_norm_params 
  * Microscaled 4-bit floating point: 32 values that follow each other along a product's contraction share a scale
  * 2^E, E = max(floor(log2(largest magnitude)) - 2, -127), held as the byte E + 127; a value is held as the nearest of 0, 0.5, 1, 1.5, 2,
  * 3, 4, 6 times the scale (codes 0 .. 7; ties to the even code, magnitudes past 6 as 6; bit 3: the sign).  A block with an
- * infinity or NaN: byte 255, which stands for 32 NaN.  Products multiply the held values exactly and add in fp32. */
+ * infinity or NaN: byte 255, which stands for 32 NaN.  Products multiply the held values exactly and add in fp32.
+ * Base pointers 16-byte aligned (BIGMAC_ERR_INVALID_ARG else).  Past 1024 groups, 2^30 rows, 2^24 columns, or 2^24 workgroups in a
+ * launch: BIGMAC_ERR_TOO_LARGE. */
 
 /* Rows (operands of a product on the left): codes [rows, cols / 2], value 2i in the low half of byte i; scales [rows,
  * bigmac_mx_scale_bytes(cols)]: 8 bytes per 256 columns, block b of them at byte (b % 2) * 4 + b / 2, unused bytes 0.  cols a multiple
@@ -369,7 +371,7 @@ int bigmac_mx_dequantize(int64_t rows, int64_t cols, const void *codes, const vo
 
 /* Weights [groups, n_in, n_out] (blocks along n_in) laid out for the matrix instructions, codes and scales in one buffer of
  * bigmac_mx_packed_bytes: done once, when the weights are loaded.  Unpacking gives the held values back.  n_in, n_out multiples
- * of 64, up to 1024 groups (past it BIGMAC_ERR_TOO_LARGE).  bigmac_mx_packed_bytes: host only, 0 for bad sizes. */
+ * of 64.  bigmac_mx_packed_bytes: host only, 0 for bad sizes. */
 size_t bigmac_mx_packed_bytes(int32_t groups, int32_t n_in, int32_t n_out);
 int bigmac_mx_pack(int32_t groups, int32_t n_in, int32_t n_out, int32_t dtype, const void *w, void *packed, void *stream);
 int bigmac_mx_unpack(int32_t groups, int32_t n_in, int32_t n_out, const void *packed, int32_t dtype, void *w, void *stream);
@@ -387,7 +389,7 @@ int bigmac_mx_product(const bigmac_mx_dims *dims, const void *codes, const void 
                       const void *bias, void *out, void *ws, size_t ws_bytes, void *stream);
 
 /* bigmac_grouped_ffn with the experts' matrices in 4 bits: the rows of x_perm are quantised, multiplied by w1, then bias, activation (fp32),
- * the hidden rows quantised from fp32, multiplied by w2, bias, o_perm in bf16.  dtype BIGMAC_BF16 only (BIGMAC_ERR_UNSUPPORTED); w1 packed
+ * the hidden rows quantised from fp32 (blocks whose scale would be under 2^-126: with that), multiplied by w2, bias, o_perm in bf16.  dtype BIGMAC_BF16 only (BIGMAC_ERR_UNSUPPORTED); w1 packed
  * [N, win, hid], w2 packed [N, hid, win]; b1, b2 as there.  ws: BIGMAC_WS_MX_GROUPED_FFN.  Rows at or past expert_offsets[N] of o_perm
  * are left as they were. */
 int bigmac_mx_grouped_ffn(const bigmac_dims *dims, const void *x_perm, const int32_t *expert_offsets, const void *w1, const void *w2,

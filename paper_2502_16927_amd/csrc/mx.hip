@@ -228,14 +228,14 @@ __global__ __launch_bounds__(256) void mx_unpack_kernel(const uint8_t* __restric
 }
 
 struct RowGrid {
-  unsigned blocks;
+  long blocks;
   int log_tx;
 };
 RowGrid row_grid(long rows, long pieces) {
   int log_tx = 2;
   while (log_tx < 8 && (1l << log_tx) < pieces) ++log_tx;
   const long per_block = (long)ROW_TURNS * (256 >> log_tx);
-  return {(unsigned)((rows + per_block - 1) / per_block), log_tx};
+  return {(rows + per_block - 1) / per_block, log_tx};
 }
 
 bool aligned(std::initializer_list<const void*> ps) {
@@ -243,21 +243,20 @@ bool aligned(std::initializer_list<const void*> ps) {
     if ((size_t)q & 15) return false;
   return true;
 }
-constexpr long MAX_ROWS = 0x7FFFFFFFl, MAX_COLS = 1l << 24;
+constexpr long MAX_ROWS = 1l << 30, MAX_COLS = 1l << 24;
 int check_rows(int64_t rows, int64_t cols, int dtype) {
   if (rows < 1 || cols < 32 || cols % 32 || (dtype != BIGMAC_F32 && dtype != BIGMAC_BF16)) return BIGMAC_ERR_INVALID_ARG;
-  return rows > MAX_ROWS || cols > MAX_COLS ? BIGMAC_ERR_TOO_LARGE : BIGMAC_OK;
+  return rows > MAX_ROWS || cols > MAX_COLS || row_grid(rows, cols / 8).blocks >= MX_MAX_BLOCKS ? BIGMAC_ERR_TOO_LARGE : BIGMAC_OK;
 }
+long pack_blocks(long groups, long n_in, long n_out) { return (groups * ((n_in + MX_CHUNK - 1) / MX_CHUNK) * 2 * (n_out / 4) + 255) / 256; }
 int check_weights(int32_t groups, int32_t n_in, int32_t n_out) {
   if (groups < 1 || n_in < 64 || n_in % 64 || n_out < 64 || n_out % 64) return BIGMAC_ERR_INVALID_ARG;
-  return groups > 1024 || n_in > MAX_COLS || n_out > MAX_COLS ? BIGMAC_ERR_TOO_LARGE : BIGMAC_OK;
-}
-unsigned pack_blocks(long groups, long n_in, long n_out) {
-  return (unsigned)((groups * ((n_in + MX_CHUNK - 1) / MX_CHUNK) * 2 * (n_out / 4) + 255) / 256);
+  return groups > 1024 || n_in > MAX_COLS || n_out > MAX_COLS || pack_blocks(groups, n_in, n_out) > MX_MAX_BLOCKS ? BIGMAC_ERR_TOO_LARGE : BIGMAC_OK;
 }
 int check_mx(const bigmac_mx_dims* D) {
   if (!D || D->rows < 1 || (D->out_dtype != BIGMAC_F32 && D->out_dtype != BIGMAC_BF16)) return BIGMAC_ERR_INVALID_ARG;
-  return check_weights(D->groups, D->n_in, D->n_out);
+  const int rc = check_weights(D->groups, D->n_in, D->n_out);
+  return rc ? rc : D->rows > MAX_ROWS ? BIGMAC_ERR_TOO_LARGE : BIGMAC_OK;
 }
 size_t mx_map_bytes(int rows, int groups) { return align_up(mx_map_ints(rows, groups) * 4); }
 
@@ -283,7 +282,7 @@ int launch_mx_quantize(long rows, long cols, int dtype, const void* src, uint8_t
   const int scale_bytes = (int)mx_scale_bytes(cols);
   const RowGrid g = row_grid(rows, cols / 8);
   const MxMapJob job = map ? *map : MxMapJob{};
-  const unsigned blocks = g.blocks + (map ? 1 : 0);
+  const unsigned blocks = (unsigned)g.blocks + (map ? 1 : 0);
   if (dtype == BIGMAC_BF16) mx_quantize_kernel<bf16_t><<<blocks, 256, 0, s>>>((const bf16_t*)src, codes, scales, rows, (int)cols, g.log_tx, scale_bytes, job);
   else mx_quantize_kernel<float><<<blocks, 256, 0, s>>>((const float*)src, codes, scales, rows, (int)cols, g.log_tx, scale_bytes, job);
   BIGMAC_CHECK_LAUNCH();
@@ -318,8 +317,8 @@ int bigmac_mx_dequantize(int64_t rows, int64_t cols, const void* codes, const vo
   const int scale_bytes = (int)mx_scale_bytes(cols);
   const RowGrid g = row_grid(rows, cols / 8);
   hipStream_t s = (hipStream_t)stream;
-  if (dtype == BIGMAC_BF16) mx_dequantize_kernel<bf16_t><<<g.blocks, 256, 0, s>>>((const uint8_t*)codes, (const uint8_t*)scales, (bf16_t*)dst, rows, (int)cols, g.log_tx, scale_bytes);
-  else mx_dequantize_kernel<float><<<g.blocks, 256, 0, s>>>((const uint8_t*)codes, (const uint8_t*)scales, (float*)dst, rows, (int)cols, g.log_tx, scale_bytes);
+  if (dtype == BIGMAC_BF16) mx_dequantize_kernel<bf16_t><<<(unsigned)g.blocks, 256, 0, s>>>((const uint8_t*)codes, (const uint8_t*)scales, (bf16_t*)dst, rows, (int)cols, g.log_tx, scale_bytes);
+  else mx_dequantize_kernel<float><<<(unsigned)g.blocks, 256, 0, s>>>((const uint8_t*)codes, (const uint8_t*)scales, (float*)dst, rows, (int)cols, g.log_tx, scale_bytes);
   BIGMAC_CHECK_LAUNCH();
   return BIGMAC_OK;
 }
@@ -328,7 +327,7 @@ int bigmac_mx_pack(int32_t groups, int32_t n_in, int32_t n_out, int32_t dtype, c
   const int rc = check_weights(groups, n_in, n_out);
   if (rc) return rc;
   if ((dtype != BIGMAC_F32 && dtype != BIGMAC_BF16) || !w || !packed || !aligned({w, packed})) return BIGMAC_ERR_INVALID_ARG;
-  const unsigned blocks = pack_blocks(groups, n_in, n_out);
+  const unsigned blocks = (unsigned)pack_blocks(groups, n_in, n_out);
   hipStream_t s = (hipStream_t)stream;
   if (dtype == BIGMAC_BF16) mx_pack_kernel<bf16_t><<<blocks, 256, 0, s>>>((const bf16_t*)w, (uint8_t*)packed, groups, n_in, n_out);
   else mx_pack_kernel<float><<<blocks, 256, 0, s>>>((const float*)w, (uint8_t*)packed, groups, n_in, n_out);
@@ -340,7 +339,7 @@ int bigmac_mx_unpack(int32_t groups, int32_t n_in, int32_t n_out, const void* pa
   const int rc = check_weights(groups, n_in, n_out);
   if (rc) return rc;
   if ((dtype != BIGMAC_F32 && dtype != BIGMAC_BF16) || !w || !packed || !aligned({w, packed})) return BIGMAC_ERR_INVALID_ARG;
-  const unsigned blocks = pack_blocks(groups, n_in, n_out);
+  const unsigned blocks = (unsigned)pack_blocks(groups, n_in, n_out);
   hipStream_t s = (hipStream_t)stream;
   if (dtype == BIGMAC_BF16) mx_unpack_kernel<bf16_t><<<blocks, 256, 0, s>>>((const uint8_t*)packed, (bf16_t*)w, groups, n_in, n_out);
   else mx_unpack_kernel<float><<<blocks, 256, 0, s>>>((const uint8_t*)packed, (float*)w, groups, n_in, n_out);
@@ -368,6 +367,10 @@ int bigmac_mx_product(const bigmac_mx_dims* D, const void* codes, const void* sc
     if (ws_bytes < mx_map_bytes(D->rows, D->groups)) return BIGMAC_ERR_WORKSPACE;
     p.offsets = offsets;
     p.tile_map = (const int*)ws;
+  }
+  rc = check_mx_product(p);
+  if (rc) return rc;
+  if (offsets) {
     mx_map_kernel<<<1, 256, 0, s>>>(MxMapJob{offsets, (int*)ws, D->groups, p.tile_rows});
     BIGMAC_CHECK_LAUNCH();
   }
@@ -381,6 +384,7 @@ int bigmac_mx_grouped_ffn(const bigmac_dims* D, const void* x_perm, const int32_
   if (D->dtype != BIGMAC_BF16) return BIGMAC_ERR_UNSUPPORTED;
   const Widths W = widths(*D);
   rc = check_weights(D->N, W.win, W.hid);
+  if (!rc) rc = check_rows((int64_t)D->T * D->k, W.win, BIGMAC_BF16);
   if (rc) return rc;
   if (!x_perm || !expert_offsets || !w1 || !w2 || !o_perm || !ws || !aligned({x_perm, w1, w2, b1, b2, o_perm, ws})) return BIGMAC_ERR_INVALID_ARG;
   const FfnPlan plan = plan_ffn(*D);
@@ -389,19 +393,22 @@ int bigmac_mx_grouped_ffn(const bigmac_dims* D, const void* x_perm, const int32_
   const int rows = (int)((long)D->T * D->k);
   uint8_t* base = (uint8_t*)ws;
   const MxMapJob map{expert_offsets, (int*)(base + plan.map), D->N, mx_tile_rows(rows, D->N, std::min(W.win, W.hid))};
+  MxProduct up{}, down{};
+  up.codes = base + plan.x_codes; up.scales = base + plan.x_scales; up.packed = (const uint8_t*)w1; up.bias = (const bf16_t*)b1;
+  up.out = base + plan.h_codes; up.out_scales = base + plan.h_scales;
+  up.n_in = W.win; up.n_out = W.hid; up.epilogue = MX_GELU_CODES;
+  down.codes = base + plan.h_codes; down.scales = base + plan.h_scales; down.packed = (const uint8_t*)w2; down.bias = (const bf16_t*)b2;
+  down.out = o_perm;
+  down.n_in = W.hid; down.n_out = W.win; down.epilogue = MX_STORE_BF16;
+  for (MxProduct* p : {&up, &down}) {
+    p->offsets = expert_offsets; p->tile_map = map.map; p->tile_rows = map.tile_rows;
+    p->rows = rows; p->groups = D->N;
+    rc = check_mx_product(*p);
+    if (rc) return rc;
+  }
   rc = launch_mx_quantize(rows, W.win, BIGMAC_BF16, x_perm, base + plan.x_codes, base + plan.x_scales, s, &map);
-  if (rc) return rc;
-  MxProduct p{};
-  p.codes = base + plan.x_codes; p.scales = base + plan.x_scales; p.packed = (const uint8_t*)w1; p.bias = (const bf16_t*)b1;
-  p.offsets = expert_offsets; p.tile_map = map.map; p.tile_rows = map.tile_rows;
-  p.out = base + plan.h_codes; p.out_scales = base + plan.h_scales;
-  p.rows = rows; p.groups = D->N; p.n_in = W.win; p.n_out = W.hid; p.epilogue = MX_GELU_CODES;
-  rc = launch_mx_product(p, s);
-  if (rc) return rc;
-  p.codes = base + plan.h_codes; p.scales = base + plan.h_scales; p.packed = (const uint8_t*)w2; p.bias = (const bf16_t*)b2;
-  p.out = o_perm; p.out_scales = nullptr;
-  p.n_in = W.hid; p.n_out = W.win; p.epilogue = MX_STORE_BF16;
-  return launch_mx_product(p, s);
+  if (!rc) rc = launch_mx_product(up, s);
+  return rc ? rc : launch_mx_product(down, s);
 }
 
 }  // extern "C"

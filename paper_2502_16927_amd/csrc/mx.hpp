@@ -50,6 +50,8 @@ __device__ __forceinline__ void mx_values8(unsigned codes, float scale, float* f
   v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.0f, 3); f[6] = v.x * scale; f[7] = v.y * scale;
 }
 
+constexpr long MX_MAX_BLOCKS = 0xFFFFFF;   // of 256 threads: a launch has under 2^32 threads
+
 enum MxEpilogue { MX_STORE_BF16 = 0, MX_STORE_F32 = 1, MX_GELU_CODES = 2 };
 // C = A W[group] (+ bias[group]) over ragged or dense rows
 struct MxProduct {
@@ -64,6 +66,7 @@ struct MxProduct {
   int tile_rows;                   // from mx_tile_rows, as the tile map's
 };
 int mx_tile_rows(int rows, int groups, int n_out);
+int check_mx_product(const MxProduct& p);   // BIGMAC_ERR_TOO_LARGE where its launch would be; before anything is launched
 int launch_mx_product(const MxProduct& p, hipStream_t s);
 // The row tiles of a ragged product: map[0] = how many, then from map[2] on (group, first row) of each, groups in order
 struct MxMapJob {

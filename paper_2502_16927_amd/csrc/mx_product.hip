@@ -409,16 +409,16 @@ __global__ __launch_bounds__(256, MT == 4 ? 2 : 4) void mx_product_kernel(MxProd
   mx_tile_product<MT, NS, EPI>(p, t, ring, staging, out_scales);
 }
 
-// Few tiles, long rows: MT x 32 rows x 64 columns per workgroup, its four wavefronts each a quarter of the inputs, their sums joined in
-// the LDS in the wavefronts' order.  With as many workgroups as fill the chip at 64 columns a row tile's operands are re-read four
-// times as often as at 256, but nothing waits for a serial walk over all inputs.  Both operands go straight to registers, a chunk ahead; no
-// barrier before the join.
-template <int MT, int EPI>
+// Few tiles, long rows: 32 rows x 64 columns per workgroup, its four wavefronts each a quarter of the inputs, their sums joined in the
+// LDS in the wavefronts' order.  With 64 columns a row tile's operands are re-read four times as often as with 256, but nothing waits for a
+// serial walk over all inputs.  Both operands go straight to registers, a chunk ahead; no barrier before the join.
+template <int EPI>
 __global__ __launch_bounds__(256, 2) void mx_split_kernel(MxProduct p) {
-  constexpr int BM = MT * 32, NS = 2;
-  __shared__ float join[3][MT * NS * 16][64];
+  constexpr int NS = 2;
+  __shared__ float join[3][NS * 16][64];
+  __shared__ uint4 staging[4096 / 16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const MxTile t = mx_tile<BM, NS>(p);
+  const MxTile t = mx_tile<32, NS>(p);
   if (!t.valid) return;
   const int strips = p.n_out / 32, steps = p.n_in / MX_STEP, chunks = (steps + 3) / 4;
   const unsigned row_bytes = (unsigned)p.n_in / 2, scale_bytes = (unsigned)chunks * 8;
@@ -427,14 +427,11 @@ __global__ __launch_bounds__(256, 2) void mx_split_kernel(MxProduct p) {
   const unsigned strip_bytes = (unsigned)mx_strip_bytes(p.n_in), scales_at = (unsigned)steps * 1024u;   // of a strip of the weights
   __amdgpu_buffer_rsrc_t bw[NS];
 #pragma unroll
-  for (int j = 0; j < NS; ++j) {
-    const size_t strip = (size_t)t.group * strips + t.strip0 + j;
-    bw[j] = scalar_buffer((size_t)p.packed + strip * strip_bytes, strip_bytes);
-  }
+  for (int j = 0; j < NS; ++j) bw[j] = scalar_buffer((size_t)p.packed + ((size_t)t.group * strips + t.strip0 + j) * strip_bytes, strip_bytes);
   const unsigned a_off = (unsigned)(lane & 31) * row_bytes + ((unsigned)lane >> 5) * 16u, s_off = (unsigned)(lane & 31) * scale_bytes + ((unsigned)lane >> 5) * 4u;
   struct Chunk {
-    u32x4_t w[NS][4], a[MT][4];
-    unsigned ws[NS], as[MT];
+    u32x4_t w[NS][4], a[4];
+    unsigned ws[NS], as;
   };
   // (past the last input: weights out of range, zeros; the rows' codes are another row's, their scales are cut off below)
   auto load = [&](Chunk& c, int chunk) {
@@ -442,30 +439,25 @@ __global__ __launch_bounds__(256, 2) void mx_split_kernel(MxProduct p) {
     for (int j = 0; j < NS; ++j) {
       c.ws[j] = __builtin_amdgcn_raw_buffer_load_b32(bw[j], scales_at + (unsigned)chunk * 256u + lane * 4u, 0, 0);
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks) c.w[j][ks] = __builtin_amdgcn_raw_buffer_load_b128(bw[j], chunk * 4 + ks < steps ? (unsigned)(chunk * 4 + ks) * 1024u + lane * 16u : 0x80000000u, 0, 0);
+      for (int ks = 0; ks < 4; ++ks)
+        c.w[j][ks] = __builtin_amdgcn_raw_buffer_load_b128(bw[j], chunk * 4 + ks < steps ? (unsigned)(chunk * 4 + ks) * 1024u + lane * 16u : 0x80000000u, 0, 0);
     }
+    c.as = __builtin_amdgcn_raw_buffer_load_b32(bs, s_off + (unsigned)chunk * 8u, 0, 0);
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      c.as[i] = __builtin_amdgcn_raw_buffer_load_b32(bs, s_off + i * 32u * scale_bytes + (unsigned)chunk * 8u, 0, 0);
-#pragma unroll
-      for (int ks = 0; ks < 4; ++ks) c.a[i][ks] = __builtin_amdgcn_raw_buffer_load_b128(ba, a_off + i * 32u * row_bytes + (unsigned)chunk * 128u + ks * 32u, 0, 0);
-    }
+    for (int ks = 0; ks < 4; ++ks) c.a[ks] = __builtin_amdgcn_raw_buffer_load_b128(ba, a_off + (unsigned)chunk * 128u + ks * 32u, 0, 0);
   };
-  f32x16_t acc[MT][NS];
+  f32x16_t acc[NS];
 #pragma unroll
-  for (int i = 0; i < MT; ++i)
-#pragma unroll
-    for (int j = 0; j < NS; ++j) acc[i][j] = f32x16_t{0};
+  for (int j = 0; j < NS; ++j) acc[j] = f32x16_t{0};
   const unsigned last_mask = steps & 3 ? (1u << (8 * (steps & 3))) - 1u : ~0u;   // (a scale byte of 255 there would make NaN of the weights' zeros)
   auto multiply = [&](const Chunk& c, int chunk) {
-    static_for<0, MT * NS>([&](auto n) {
-      constexpr int i = decltype(n)::value / NS, j = decltype(n)::value % NS;
-      const unsigned as = chunk + 1 == chunks ? c.as[i] & last_mask : c.as[i];
-      static_for<0, 4>([&](auto ks) { acc[i][j] = mx_mfma<decltype(ks)::value>(c.w[j][decltype(ks)::value], c.ws[j], c.a[i][decltype(ks)::value], as, acc[i][j]); });
+    const unsigned as = chunk + 1 == chunks ? c.as & last_mask : c.as;
+    static_for<0, NS>([&](auto n) {
+      constexpr int j = decltype(n)::value;
+      static_for<0, 4>([&](auto ks) { acc[j] = mx_mfma<decltype(ks)::value>(c.w[j][decltype(ks)::value], c.ws[j], c.a[decltype(ks)::value], as, acc[j]); });
     });
   };
-  // this wavefront's chunks
-  const int first = chunks * wave / 4, last = chunks * (wave + 1) / 4;
+  const int first = chunks * wave / 4, last = chunks * (wave + 1) / 4;            // this wavefront's chunks
   Chunk one, two;
   if (first < last) {
     load(one, first);
@@ -480,36 +472,29 @@ __global__ __launch_bounds__(256, 2) void mx_split_kernel(MxProduct p) {
   }
   if (wave > 0)
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+    for (int j = 0; j < NS; ++j)
 #pragma unroll
-      for (int j = 0; j < NS; ++j)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) join[wave - 1][(i * NS + j) * 16 + v][lane] = acc[i][j][v];
+      for (int v = 0; v < 16; ++v) join[wave - 1][j * 16 + v][lane] = acc[j][v];
   __syncthreads();
   if (wave > 0) return;
+#pragma unroll
+  for (int w = 0; w < 3; ++w)
+#pragma unroll
+    for (int j = 0; j < NS; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[j][v] += join[w][j * 16 + v][lane];
   float bias[NS][16];
   mx_bias<NS>(p, t, t.strip0, bias, lane);
-  __shared__ uint4 staging[4096 / 16];
-#pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    if (i * 32 >= t.m_rows) break;
-#pragma unroll
-    for (int w = 0; w < 3; ++w)
-#pragma unroll
-      for (int j = 0; j < NS; ++j)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) acc[i][j][v] += join[w][(i * NS + j) * 16 + v][lane];
-    if constexpr (EPI == MX_GELU_CODES) {
-      unsigned bytes[NS];
-      const uint4 block = mx_gelu_blocks<NS>(acc[i], bias, p.bias != nullptr, bytes);
-      const int row = i * 32 + (lane & 31);
-      if (row < t.m_rows) {
-        *(uint4*)((uint8_t*)p.out + (size_t)(t.m0 + row) * (p.n_out / 2) + (size_t)(t.strip0 + (lane >> 5)) * 16) = block;
-        p.out_scales[(size_t)(t.m0 + row) * ((p.n_out + MX_CHUNK - 1) / MX_CHUNK * 8) + mx_scale_at(t.strip0 + (lane >> 5))] = (uint8_t)(lane < 32 ? bytes[0] : bytes[1]);
-      }
-    } else {
-      mx_store<NS>(p, acc[i], bias, t.m0 + i * 32, t.m_rows - i * 32, t.strip0 * 32, (char*)staging, lane, std::integral_constant<int, EPI>{});
+  if constexpr (EPI == MX_GELU_CODES) {
+    unsigned bytes[NS];
+    const uint4 block = mx_gelu_blocks<NS>(acc, bias, p.bias != nullptr, bytes);
+    const int row = lane & 31, strip = t.strip0 + (lane >> 5);
+    if (row < t.m_rows) {
+      *(uint4*)((uint8_t*)p.out + (size_t)(t.m0 + row) * (p.n_out / 2) + (size_t)strip * 16) = block;
+      p.out_scales[(size_t)(t.m0 + row) * ((p.n_out + MX_CHUNK - 1) / MX_CHUNK * 8) + mx_scale_at(strip)] = (uint8_t)(lane < 32 ? bytes[0] : bytes[1]);
     }
+  } else {
+    mx_store<NS>(p, acc, bias, t.m0, t.m_rows, t.strip0 * 32, (char*)staging, lane, std::integral_constant<int, EPI>{});
   }
 }
 
@@ -517,26 +502,27 @@ __global__ __launch_bounds__(256, 2) void mx_split_kernel(MxProduct p) {
 long most_tiles(const MxProduct& p, int tile_rows) {
   return p.offsets ? (long)p.rows / tile_rows + std::min(p.groups, p.rows) : ((long)p.rows + tile_rows - 1) / tile_rows;
 }
+// A quarter of the inputs per wavefront, for few tiles and a long walk: us without and with at 4096 inputs, 1024 columns: 1 row 8.4, 6.1;
+// 500 (64 tiles of 256 columns) 10.0, 8.3; 8 groups of 32 (32) 12.8, 10.9; 16 of 16 (64) 13.2, 12.3; 8 of 125 (128) 13.1, 15.6; at 1024 inputs within 0.4.
+long even_tiles(long rows, long groups, int tile_rows) {   // rows spread evenly over the groups
+  const long busy = std::min(rows, groups), each = (rows + busy - 1) / busy;
+  return busy * ((each + tile_rows - 1) / tile_rows);
+}
+bool splits(const MxProduct& p) { return p.tile_rows == 32 && p.n_in >= 2048 && even_tiles(p.rows, p.groups, 32) * ((p.n_out + 255) / 256) <= 64; }
+long product_blocks(const MxProduct& p) {
+  const int columns = splits(p) ? 64 : 256;
+  return (most_tiles(p, p.tile_rows) * ((p.n_out + columns - 1) / columns) + 7) / 8 * 8;
+}
 template <int MT>
-int launch_of(const MxProduct& p, hipStream_t s) {
-  const long gx = (p.n_out + 255) / 256, blocks = (most_tiles(p, MT * 32) * gx + 7) / 8 * 8;
-  if (blocks > 0x3FFFFFFFl) return BIGMAC_ERR_TOO_LARGE;
-  const dim3 grid((unsigned)blocks);
+void launch_of(const MxProduct& p, dim3 grid, hipStream_t s) {
   if (p.epilogue == MX_GELU_CODES) mx_product_kernel<MT, 2, MX_GELU_CODES><<<grid, 256, 0, s>>>(p);
   else if (p.epilogue == MX_STORE_F32) mx_product_kernel<MT, 2, MX_STORE_F32><<<grid, 256, 0, s>>>(p);
   else mx_product_kernel<MT, 2, MX_STORE_BF16><<<grid, 256, 0, s>>>(p);
-  BIGMAC_CHECK_LAUNCH();
-  return BIGMAC_OK;
 }
-int launch_split(const MxProduct& p, hipStream_t s) {
-  const long blocks = (most_tiles(p, 32) * (p.n_out / 64) + 7) / 8 * 8;
-  if (blocks > 0x3FFFFFFFl) return BIGMAC_ERR_TOO_LARGE;
-  const dim3 grid((unsigned)blocks);
-  if (p.epilogue == MX_GELU_CODES) mx_split_kernel<1, MX_GELU_CODES><<<grid, 256, 0, s>>>(p);
-  else if (p.epilogue == MX_STORE_F32) mx_split_kernel<1, MX_STORE_F32><<<grid, 256, 0, s>>>(p);
-  else mx_split_kernel<1, MX_STORE_BF16><<<grid, 256, 0, s>>>(p);
-  BIGMAC_CHECK_LAUNCH();
-  return BIGMAC_OK;
+void launch_split(const MxProduct& p, dim3 grid, hipStream_t s) {
+  if (p.epilogue == MX_GELU_CODES) mx_split_kernel<MX_GELU_CODES><<<grid, 256, 0, s>>>(p);
+  else if (p.epilogue == MX_STORE_F32) mx_split_kernel<MX_STORE_F32><<<grid, 256, 0, s>>>(p);
+  else mx_split_kernel<MX_STORE_BF16><<<grid, 256, 0, s>>>(p);
 }
 
 }  // namespace
@@ -546,18 +532,17 @@ int launch_split(const MxProduct& p, hipStream_t s) {
 // on both sides, us with 128 and 32 rows: 1024 dense rows 4096 -> 1024 (32 tiles) 15.6, 10.2; 2048 (64) 16.2, 11.5; 4096 (128) 17.2, 19.0;
 // 2048 rows 1024 -> 4096 (256) 10.8, 12.9; 8 groups of 250 rows 4096 -> 1024 (64) 19.2, 14.7; 1024 -> 4096 of 8 x 125 (128) 11.4, 11.5.
 // n_out: of the narrowest product that walks the tiles.
-long even_tiles(long rows, long groups, int tile_rows) {
-  const long busy = std::min(rows, groups), each = (rows + busy - 1) / busy;
-  return busy * ((each + tile_rows - 1) / tile_rows);
-}
 int mx_tile_rows(int rows, int groups, int n_out) { return even_tiles(rows, groups, 128) * ((n_out + 255) / 256) < 128 ? 32 : 128; }
 
+int check_mx_product(const MxProduct& p) { return product_blocks(p) > MX_MAX_BLOCKS ? BIGMAC_ERR_TOO_LARGE : BIGMAC_OK; }
+
 int launch_mx_product(const MxProduct& p, hipStream_t s) {
-  if (p.tile_rows == 128) return launch_of<4>(p, s);
-  // A quarter of the inputs per wavefront, for few tiles and a long walk: us without and with at 4096 inputs, 1024 columns: 1 row 8.4, 6.1;
-  // 500 (64 tiles of 256 columns) 10.0, 8.3; 8 groups of 32 (32) 12.8, 10.9; 16 of 16 (64) 13.2, 12.3; 8 of 125 (128) 13.1, 15.6; at 1024 inputs within 0.4
-  if (p.n_in >= 2048 && even_tiles(p.rows, p.groups, 32) * ((p.n_out + 255) / 256) <= 64) return launch_split(p, s);
-  return launch_of<1>(p, s);
+  const dim3 grid((unsigned)product_blocks(p));
+  if (splits(p)) launch_split(p, grid, s);
+  else if (p.tile_rows == 128) launch_of<4>(p, grid, s);
+  else launch_of<1>(p, grid, s);
+  BIGMAC_CHECK_LAUNCH();
+  return BIGMAC_OK;
 }
 
 }  // namespace bigmac

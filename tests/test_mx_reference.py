@@ -53,6 +53,7 @@ def test_sizes_and_refusals():
     for bad in (dict(codes=None), dict(scales=None), dict(offsets=None), dict(packed=None), dict(out=None), dict(ws=None), dict(codes=odd), dict(bias=odd), dict(out=odd), dict(ws=odd)):
         assert product(d, **bad) == -1, bad
     assert product(d, ws_bytes=B.mx_workspace_bytes(d) - 1) == -2
+    assert product(B.make_mx_dims((1 << 30) + 1, 1, 64, 64)) == -5 and product(B.make_mx_dims(1 << 30, 1, 64, 1 << 20)) == -5    # rows; workgroups
     assert product(B.make_mx_dims(0, 4, 128, 64)) == -1 and product(B.make_mx_dims(9, 4, 128, 64, 2)) == -1
 
     def ffn(d, x=fake, offsets=fake, w1=fake, w2=fake, b1=None, b2=None, out=fake, ws=fake, ws_bytes=1 << 40):
