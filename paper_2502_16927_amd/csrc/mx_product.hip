@@ -33,8 +33,8 @@ __device__ __forceinline__ void lds_read_b32(unsigned addr, unsigned& v) { asm v
 
 // GELU for 4-bit results: a polynomial of degree 5 for log2 of the normal tail (minimax of the tail's absolute error, of |a| times it past
 // 1: under 7e-7, so within 7e-7 of |a| and of 1; the smallest step of a 4-bit value is an eighth of it or more).  It falls without end, so |a|
-// needs no limit.  max(a, 0) on the bits as an integer: one instruction.  The vector ALU is what bounds a product with this epilogue (the
-// 131072 x 4096 hidden values of a 16384-token call: each instruction per value is 17 us).
+// needs no limit.  max(a, 0) on the bits as an integer: one instruction.  The vector ALU is what bounds a product with this epilogue: for
+// the 131072 x 4096 hidden values of a 16384-token call every instruction per value is 16 us, and a matrix instruction leaves it about half of its time.
 __device__ __forceinline__ float gelu_mx_f(float a) {
   const float x = fabsf(a);
   float q = fmaf(x, -5.002595082e-04f, 7.282377832e-03f);
@@ -191,8 +191,15 @@ __device__ __forceinline__ void mx_bias(const MxProduct& p, const MxTile& t, int
 //
 // Weights go from memory to registers as they lie there (1 KB per instruction operand, whole lines), each wavefront its own columns'.
 // Rows go straight to the LDS in chunks of 256 inputs, three stages: while chunk c is multiplied, chunk c + 1 has landed or is about
-// to and chunk c + 2 is requested.  A chunk's step: the eight (MT NS) instructions of 64 inputs, between them the LDS reads of the next
+// to and chunk c + 2 is requested.  A chunk's step: the MT NS instructions of 64 inputs, between them the LDS reads of the next
 // step's fragments, behind them the next chunk's weights of the same step, into the registers that have just been read.
+//
+// What bounds it, at 131072 rows, 1024 -> 4096 with GELU and 4096 -> 1024 without (389 and 304 us, 2.8 and 3.6 PFLOP/s, matrix cores busy 31
+// and 39 % at 2.2 GHz): without the epilogues 259 and 270 us (53 % at 1.9 GHz), without the loop's requests too 190 (78 % at
+// 1.8 GHz), without its LDS reads too 160: power holds the clock down, and the requests cost as much as the epilogue.  Two workgroups share a CU.
+// Slower or level: one persistent workgroup walking many tiles with its operands requested a tile ahead (917 us a 16384-token call against 873),
+// 256 x 256 tiles by eight wavefronts (960 against 819), 64-row tiles (885 against 797), 32 columns a wavefront (888 against 874), weights two
+// chunks ahead (807 against 796), the rows of a tile kept in the LDS for all columns (803 against 799).
 constexpr int MX_STAGES = 3;
 constexpr unsigned mx_stage_bytes(int mt) { return mt * 4096 + 1024; }   // codes; 256 dwords of scales (past the tile's rows: zeros)
 template <int MT, int NS, int EPI>

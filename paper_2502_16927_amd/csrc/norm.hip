@@ -5,9 +5,10 @@
 //     n'(c) = rstd (a - mean(a) - v^ mean(a v^))   (RMS norm: without mean(a)),   dw = sum_t c v^,   db = sum_t c
 //     dZ = dz + n_pre'(du);   dx = alpha dZ;   dn = g dZ;   dy = n_post'(dn);   dg = dZ n_post(y), summed over what g is broadcast over
 //
-// What bounds them: HBM.  A row passes through registers once: a wavefront (up to 1024 columns) or 2 to 16 of one
-// workgroup hold it, 8 or 16 elements a lane, so every tensor is read once and written once, and the statistics of the
-// backward are worked out again from the rows that it reads anyway instead of being stored.  Vectors (weights, channel
+// What bounds them: HBM.  A row passes through registers once: a wavefront (up to 512 columns) or 2 to 16 of one workgroup hold it,
+// 8 columns a lane, so every tensor is read once and written once, and the statistics of the backward are worked out again from the
+// rows that it reads anyway instead of being stored.  (16 columns a lane: 154 registers forward, 234 backward, two wavefronts a SIMD.)  32768 rows
+// of 4096, bf16 stream, fp32 y: forward 242 us (5.6 TB/s), backward 428 us (5.0 TB/s; a large copy reaches 4.9).  Vectors (weights, channel
 // gate) stay in registers over the rows of a persistent workgroup.  Sums and statistics are fp32; a layer norm's variance is
 // taken behind its mean.  Rows are addressed as buffers (range = the row): a lane past the end of the row loads zeros and its
 // stores are dropped, and the two halves of an fp32 piece and the one of a bf16 piece are the same code without a branch.
@@ -72,7 +73,7 @@ __device__ __forceinline__ void store8(__amdgpu_buffer_rsrc_t r, int col, int f3
     __builtin_amdgcn_raw_buffer_store_b128(b, r, (unsigned)col * 4u + 16u, 0, 0);
     if (rounded)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) rounded[i] = f[i];
+    for (int i = 0; i < 8; ++i) rounded[i] = f[i];
   } else {
     q4_t a;
 #pragma unroll
@@ -80,7 +81,7 @@ __device__ __forceinline__ void store8(__amdgpu_buffer_rsrc_t r, int col, int f3
     __builtin_amdgcn_raw_buffer_store_b128(a, r, (unsigned)col * 2u, 0, 0);
     if (rounded)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) rounded[i] = __uint_as_float(i & 1 ? a[i >> 1] & 0xFFFF0000u : a[i >> 1] << 16);
+    for (int i = 0; i < 8; ++i) rounded[i] = __uint_as_float(i & 1 ? a[i >> 1] & 0xFFFF0000u : a[i >> 1] << 16);
   }
 }
 
@@ -107,43 +108,34 @@ __device__ __forceinline__ void row_sums(float (&v)[M], float* box, int& turn, i
   }
 }
 
-template <int NV>
-__device__ __forceinline__ void load_vector(const float* p, int d, const int (&col)[NV], float none, float (&f)[NV][8]) {
+__device__ __forceinline__ void load_vector(const float* p, int d, int col, float none, float (&f)[8]) {
   const auto r = row_buffer(p, 0, d, 1);
+  Raw8 q;
+  q.load(r, col, 1);
+  q.values(1, f);
+  if (!p)
 #pragma unroll
-  for (int v = 0; v < NV; ++v) {
-    Raw8 q;
-    q.load(r, col[v], 1);
-    q.values(1, f[v]);
-    if (!p)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) f[v][i] = none;
-  }
+    for (int i = 0; i < 8; ++i) f[i] = none;
 }
 
-// W wavefronts per row, NV pieces of 8 columns per lane
-template <int W, int NV>
+// W wavefronts per row, 8 columns per lane
+template <int W>
 struct RowShape {
   static constexpr int WAVES = W < 4 ? 4 : W, THREADS = WAVES * 64, SLOTS = WAVES / W;   // rows a workgroup holds at a time
 };
 
-template <int W, int NV, bool POST, bool PRE>
-__global__ __launch_bounds__((RowShape<W, NV>::THREADS)) void norm_forward_kernel(NormArgs p) {
-  using S = RowShape<W, NV>;
+template <int W, bool POST, bool PRE>
+__global__ __launch_bounds__((RowShape<W>::THREADS)) void norm_forward_kernel(NormArgs p) {
+  using S = RowShape<W>;
   __shared__ float box[W > 1 ? 2 * S::SLOTS * W * 4 : 1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int slot = wave / W, wir = wave % W;
-  int col[NV];
-  float in_row[NV];
-#pragma unroll
-  for (int v = 0; v < NV; ++v) {
-    col[v] = ((v * W + wir) * 64 + lane) * 8;
-    in_row[v] = col[v] < p.d ? 1.0f : 0.0f;
-  }
-  float pw[NV][8], qw[NV][8], cg[NV][8];
-  if (POST) load_vector<NV>(p.post_w, p.d, col, 1.0f, pw);
-  if (PRE) load_vector<NV>(p.pre_w, p.d, col, 1.0f, qw);
-  if (POST) load_vector<NV>(p.gate_kind == BIGMAC_GATE_CHANNEL ? (const float*)p.gate : nullptr, p.d, col, 1.0f, cg);
+  const int col = (wir * 64 + lane) * 8;
+  const float in_row = col < p.d ? 1.0f : 0.0f;
+  float pw[8], qw[8], cg[8];
+  if (POST) load_vector(p.post_w, p.d, col, 1.0f, pw);
+  if (PRE) load_vector(p.pre_w, p.d, col, 1.0f, qw);
+  if (POST) load_vector(p.gate_kind == BIGMAC_GATE_CHANNEL ? (const float*)p.gate : nullptr, p.d, col, 1.0f, cg);
   int turn = 0;
   // every wavefront makes the same number of turns: the barriers of the sums are the workgroup's
   for (int first = blockIdx.x * S::SLOTS; first < p.T; first += gridDim.x * S::SLOTS) {
@@ -151,112 +143,88 @@ __global__ __launch_bounds__((RowShape<W, NV>::THREADS)) void norm_forward_kerne
     const bool live = row < p.T;
     const int at = live ? row : 0;
     auto buffer = [&](const void* base, int f32) { return row_buffer(live ? base : nullptr, at, p.d, f32); };
-    Raw8 rx[NV], ry[NV], rg[NV];
+    Raw8 rx, ry, rg;
     const auto bx = buffer(p.x, p.x_f32), by = buffer(p.y, p.y_f32), bg = buffer(p.gate_kind == BIGMAC_GATE_FULL ? p.gate : nullptr, p.u_f32);
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      if (POST) ry[v].load(by, col[v], p.y_f32);
-      rx[v].load(bx, col[v], p.x_f32);
-      if (POST && p.gate_kind == BIGMAC_GATE_FULL) rg[v].load(bg, col[v], p.u_f32);
-    }
+    if (POST) ry.load(by, col, p.y_f32);
+    rx.load(bx, col, p.x_f32);
+    if (POST && p.gate_kind == BIGMAC_GATE_FULL) rg.load(bg, col, p.u_f32);
     float token_gate = 1.0f;
     if (POST && p.gate_kind == BIGMAC_GATE_TOKEN) token_gate = ((const float*)p.gate)[at];
 
     // mean and reciprocal root of a row held in registers
-    auto centre = [&](float (&f)[NV][8]) {   // subtracts the mean of a layer norm, returns rstd
+    auto centre = [&](float (&f)[8]) {   // subtracts the mean of a layer norm, returns rstd
       if (p.layer) {
         float s[1] = {0.0f};
 #pragma unroll
-        for (int v = 0; v < NV; ++v)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) s[0] += f[v][i];
+        for (int i = 0; i < 8; ++i) s[0] += f[i];
         row_sums<W, 1, S::SLOTS>(s, box, turn, slot, wir, lane);
         const float m = s[0] * p.inv_d;
 #pragma unroll
-        for (int v = 0; v < NV; ++v)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) f[v][i] = in_row[v] * (f[v][i] - m);
+        for (int i = 0; i < 8; ++i) f[i] = in_row * (f[i] - m);
       }
       float s[1] = {0.0f};
 #pragma unroll
-      for (int v = 0; v < NV; ++v)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) s[0] = fmaf(f[v][i], f[v][i], s[0]);
+      for (int i = 0; i < 8; ++i) s[0] = fmaf(f[i], f[i], s[0]);
       row_sums<W, 1, S::SLOTS>(s, box, turn, slot, wir, lane);
       return 1.0f / sqrtf(fmaf(s[0], p.inv_d, p.eps));
     };
-    auto affine = [&](float (&f)[NV][8], float rstd, const float (&w)[NV][8], const float* bias) {
-      float b[NV][8];
-      if (bias) load_vector<NV>(bias, p.d, col, 0.0f, b);
+    auto affine = [&](float (&f)[8], float rstd, const float (&w)[8], const float* bias) {
+      float b[8];
+      if (bias) load_vector(bias, p.d, col, 0.0f, b);
 #pragma unroll
-      for (int v = 0; v < NV; ++v)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[v][i] = bias ? fmaf(f[v][i] * rstd, w[v][i], b[v][i]) : f[v][i] * rstd * w[v][i];
+      for (int i = 0; i < 8; ++i) f[i] = bias ? fmaf(f[i] * rstd, w[i], b[i]) : f[i] * rstd * w[i];
     };
 
-    float z[NV][8];
+    float z[8];
     if (POST) {
-      float n[NV][8];
-#pragma unroll
-      for (int v = 0; v < NV; ++v) ry[v].values(p.y_f32, n[v]);
+      float n[8];
+      ry.values(p.y_f32, n);
       const float rstd = centre(n);
       affine(n, rstd, pw, p.post_b);
       const auto bz = buffer(p.z, p.x_f32);
+      float f[8], g[8];
+      rx.values(p.x_f32, f);
+      if (p.gate_kind == BIGMAC_GATE_FULL) rg.values(p.u_f32, g);
 #pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        float f[8], g[8];
-        rx[v].values(p.x_f32, f);
-        if (p.gate_kind == BIGMAC_GATE_FULL) rg[v].values(p.u_f32, g);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float gate = p.gate_kind == BIGMAC_GATE_FULL ? g[i] : cg[v][i] * token_gate;
-          f[i] = fmaf(gate, n[v][i], p.alpha * f[i]);
-        }
-        store8(bz, col[v], p.x_f32, f, z[v]);
+      for (int i = 0; i < 8; ++i) {
+        const float gate = p.gate_kind == BIGMAC_GATE_FULL ? g[i] : cg[i] * token_gate;
+        f[i] = fmaf(gate, n[i], p.alpha * f[i]);
       }
+      store8(bz, col, p.x_f32, f, z);
     } else {
-#pragma unroll
-      for (int v = 0; v < NV; ++v) rx[v].values(p.x_f32, z[v]);
+      rx.values(p.x_f32, z);
     }
     if (PRE) {
-      // (columns past the row hold alpha * 0 + gate * 0, or with a bias of a NULL gate buffer 0: zero in every case)
+      // (columns past the row hold alpha * 0 + gate * 0: zero)
       const float rstd = centre(z);
       affine(z, rstd, qw, p.pre_b);
       const auto bu = buffer(p.u, p.u_f32);
-#pragma unroll
-      for (int v = 0; v < NV; ++v) store8(bu, col[v], p.u_f32, z[v]);
+      store8(bu, col, p.u_f32, z);
     }
   }
 }
 
 // Vectors of partial sums, in this order as far as the call has them: du z^, dn y^ (with a channel gate dZ y^), du, dn (dZ)
-template <int W, int NV, bool POST, bool PRE, bool BIAS>
-// (four wavefronts a SIMD where the sums leave room: 32768 x 4096 471 -> 443 us; with biases their registers spill, 43 -> 50 us at 6001 x 1024)
-__global__ __launch_bounds__((RowShape<W, NV>::THREADS), BIAS ? 1 : 4) void norm_backward_kernel(NormArgs p) {
-  using S = RowShape<W, NV>;
+// Four wavefronts a SIMD where the sums leave room: 32768 x 4096 471 -> 443 us; with biases their registers spill, 43 -> 50 us at 6001 x 1024.
+template <int W, bool POST, bool PRE, bool BIAS>
+__global__ __launch_bounds__((RowShape<W>::THREADS), BIAS ? 1 : 4) void norm_backward_kernel(NormArgs p) {
+  using S = RowShape<W>;
   constexpr int VECTORS = ((POST ? 1 : 0) + (PRE ? 1 : 0)) * (BIAS ? 2 : 1);
   __shared__ float box[W > 1 ? 2 * S::SLOTS * W * 4 : 1];
   __shared__ float4 join[S::SLOTS > 1 ? (S::SLOTS - 1) * W * 64 * 2 : 1];   // the slots' sums on their way into the first slot's, 8 columns per lane
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int slot = wave / W, wir = wave % W;
-  int col[NV];
-  float in_row[NV];
-#pragma unroll
-  for (int v = 0; v < NV; ++v) {
-    col[v] = ((v * W + wir) * 64 + lane) * 8;
-    in_row[v] = col[v] < p.d ? 1.0f : 0.0f;
-  }
-  float pw[NV][8], qw[NV][8], cg[NV][8];
-  if (POST) load_vector<NV>(p.post_w, p.d, col, 1.0f, pw);
-  if (PRE) load_vector<NV>(p.pre_w, p.d, col, 1.0f, qw);
-  if (POST) load_vector<NV>(p.gate_kind == BIGMAC_GATE_CHANNEL ? (const float*)p.gate : nullptr, p.d, col, 1.0f, cg);
-  float sum[VECTORS][NV][8];
+  const int col = (wir * 64 + lane) * 8;
+  const float in_row = col < p.d ? 1.0f : 0.0f;
+  float pw[8], qw[8], cg[8];
+  if (POST) load_vector(p.post_w, p.d, col, 1.0f, pw);
+  if (PRE) load_vector(p.pre_w, p.d, col, 1.0f, qw);
+  if (POST) load_vector(p.gate_kind == BIGMAC_GATE_CHANNEL ? (const float*)p.gate : nullptr, p.d, col, 1.0f, cg);
+  float sum[VECTORS][8];
 #pragma unroll
   for (int k = 0; k < VECTORS; ++k)
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) sum[k][v][i] = 0.0f;
+    for (int i = 0; i < 8; ++i) sum[k][i] = 0.0f;
   constexpr int AT_PRE = 0, AT_POST = PRE ? 1 : 0, AT_BIAS = (POST ? 1 : 0) + (PRE ? 1 : 0);
   int turn = 0;
   for (int first = blockIdx.x * S::SLOTS; first < p.T; first += gridDim.x * S::SLOTS) {
@@ -264,151 +232,127 @@ __global__ __launch_bounds__((RowShape<W, NV>::THREADS), BIAS ? 1 : 4) void norm
     const bool live = row < p.T;
     const int at = live ? row : 0;
     auto buffer = [&](const void* base, int f32) { return row_buffer(live ? base : nullptr, at, p.d, f32); };
-    Raw8 rz[NV], ry[NV], rdu[NV], rdz[NV], rg[NV];
+    Raw8 rz, ry, rdu, rdz, rg;
     const auto bz = buffer(p.x, p.x_f32), by = buffer(p.y, p.y_f32), bdu = buffer(p.du, p.y_f32), bdz = buffer(p.dz, p.x_f32);
     const auto bg = buffer(p.gate_kind == BIGMAC_GATE_FULL ? p.gate : nullptr, p.u_f32);
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      if (PRE) rz[v].load(bz, col[v], p.x_f32);
-      if (PRE) rdu[v].load(bdu, col[v], p.y_f32);
-      if (POST) ry[v].load(by, col[v], p.y_f32);
-      rdz[v].load(bdz, col[v], p.x_f32);
-      if (POST && p.gate_kind == BIGMAC_GATE_FULL) rg[v].load(bg, col[v], p.u_f32);
-    }
+    if (PRE) rz.load(bz, col, p.x_f32);
+    if (PRE) rdu.load(bdu, col, p.y_f32);
+    if (POST) ry.load(by, col, p.y_f32);
+    rdz.load(bdz, col, p.x_f32);
+    if (POST && p.gate_kind == BIGMAC_GATE_FULL) rg.load(bg, col, p.u_f32);
     float token_gate = 1.0f;
     if (POST && p.gate_kind == BIGMAC_GATE_TOKEN) token_gate = ((const float*)p.gate)[at];
 
-    float z[NV][8], du[NV][8], y[NV][8];
-    if (PRE)
-#pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        rz[v].values(p.x_f32, z[v]);
-        rdu[v].values(p.y_f32, du[v]);
-      }
-    if (POST)
-#pragma unroll
-      for (int v = 0; v < NV; ++v) ry[v].values(p.y_f32, y[v]);
+    float z[8], du[8], y[8];
+    if (PRE) {
+      rz.values(p.x_f32, z);
+      rdu.values(p.y_f32, du);
+    }
+    if (POST) ry.values(p.y_f32, y);
     float mean_a = 0.0f;
     if (p.layer) {   // means first: of z, of du w_pre, of y
       float s[3] = {0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int v = 0; v < NV; ++v)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          if (PRE) s[0] += z[v][i], s[1] = fmaf(du[v][i], qw[v][i], s[1]);
-          if (POST) s[2] += y[v][i];
-        }
+      for (int i = 0; i < 8; ++i) {
+        if (PRE) s[0] += z[i], s[1] = fmaf(du[i], qw[i], s[1]);
+        if (POST) s[2] += y[i];
+      }
       row_sums<W, 3, S::SLOTS>(s, box, turn, slot, wir, lane);
       mean_a = s[1] * p.inv_d;
 #pragma unroll
-      for (int v = 0; v < NV; ++v)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          if (PRE) z[v][i] = in_row[v] * (z[v][i] - s[0] * p.inv_d);
-          if (POST) y[v][i] = in_row[v] * (y[v][i] - s[2] * p.inv_d);
-        }
+      for (int i = 0; i < 8; ++i) {
+        if (PRE) z[i] = in_row * (z[i] - s[0] * p.inv_d);
+        if (POST) y[i] = in_row * (y[i] - s[2] * p.inv_d);
+      }
     }
     float s[3] = {0.0f, 0.0f, 0.0f};   // sums of squares of z and y, of du w_pre z
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if (PRE) s[0] = fmaf(z[v][i], z[v][i], s[0]), s[1] = fmaf(du[v][i] * qw[v][i], z[v][i], s[1]);
-        if (POST) s[2] = fmaf(y[v][i], y[v][i], s[2]);
-      }
+    for (int i = 0; i < 8; ++i) {
+      if (PRE) s[0] = fmaf(z[i], z[i], s[0]), s[1] = fmaf(du[i] * qw[i], z[i], s[1]);
+      if (POST) s[2] = fmaf(y[i], y[i], s[2]);
+    }
     row_sums<W, 3, S::SLOTS>(s, box, turn, slot, wir, lane);
-    float dZ[NV][8];
+    float dZ[8];
     {
       const float r = PRE && live ? 1.0f / sqrtf(fmaf(s[0], p.inv_d, p.eps)) : 0.0f;   // (no row: nothing that an eps of 0 makes infinite)
       const float c = s[1] * r * p.inv_d;   // mean(a z^)
       const auto bdx = buffer(p.dx, p.x_f32);
+      rdz.values(p.x_f32, dZ);
+      float out[8];
 #pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        rdz[v].values(p.x_f32, dZ[v]);
-        float out[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          if (PRE) {
-            const float zh = z[v][i] * r;
-            dZ[v][i] = fmaf(r, du[v][i] * qw[v][i] - mean_a - zh * c, dZ[v][i]);
-            sum[AT_PRE][v][i] = fmaf(du[v][i], zh, sum[AT_PRE][v][i]);
-            if (BIAS) sum[AT_BIAS][v][i] += du[v][i];
-          }
-          out[i] = p.alpha * dZ[v][i];
+      for (int i = 0; i < 8; ++i) {
+        if (PRE) {
+          const float zh = z[i] * r;
+          dZ[i] = fmaf(r, du[i] * qw[i] - mean_a - zh * c, dZ[i]);
+          sum[AT_PRE][i] = fmaf(du[i], zh, sum[AT_PRE][i]);
+          if (BIAS) sum[AT_BIAS][i] += du[i];
         }
-        store8(bdx, col[v], p.x_f32, out);
+        out[i] = p.alpha * dZ[i];
       }
+      store8(bdx, col, p.x_f32, out);
     }
     if (POST) {
       const float r = live ? 1.0f / sqrtf(fmaf(s[2], p.inv_d, p.eps)) : 0.0f;
       const auto bdg = buffer(p.gate_kind == BIGMAC_GATE_FULL ? p.dgate : nullptr, p.u_f32);
       float q[3] = {0.0f, 0.0f, 0.0f};   // sums of e, of e y^, of dZ n(y);  e = dn w_post
-      float b[NV][8];
-      if (BIAS) load_vector<NV>(p.post_b, p.d, col, 0.0f, b);
+      float b[8];
+      if (BIAS) load_vector(p.post_b, p.d, col, 0.0f, b);
+      float g[8], dg[8];
+      if (p.gate_kind == BIGMAC_GATE_FULL) rg.values(p.u_f32, g);
 #pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        float g[8], dg[8];
-        if (p.gate_kind == BIGMAC_GATE_FULL) rg[v].values(p.u_f32, g);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          y[v][i] *= r;
-          const float n = BIAS ? fmaf(pw[v][i], y[v][i], b[v][i]) : pw[v][i] * y[v][i];
-          dg[i] = in_row[v] * (dZ[v][i] * n);
-          q[2] += dg[i];
-          const float gate = p.gate_kind == BIGMAC_GATE_FULL ? g[i] : cg[v][i] * token_gate;
-          const float dn = gate * dZ[v][i];
-          const float counted = p.gate_kind == BIGMAC_GATE_CHANNEL ? dZ[v][i] : dn;
-          sum[AT_POST][v][i] = fmaf(counted, y[v][i], sum[AT_POST][v][i]);
-          if (BIAS) sum[AT_BIAS + (PRE ? 1 : 0)][v][i] += counted;
-          const float e = in_row[v] * (dn * pw[v][i]);
-          dZ[v][i] = e;
-          q[0] += e;
-          q[1] = fmaf(e, y[v][i], q[1]);
-        }
-        if (p.gate_kind == BIGMAC_GATE_FULL) store8(bdg, col[v], p.u_f32, dg);
+      for (int i = 0; i < 8; ++i) {
+        y[i] *= r;
+        const float n = BIAS ? fmaf(pw[i], y[i], b[i]) : pw[i] * y[i];
+        dg[i] = in_row * (dZ[i] * n);
+        q[2] += dg[i];
+        const float gate = p.gate_kind == BIGMAC_GATE_FULL ? g[i] : cg[i] * token_gate;
+        const float dn = gate * dZ[i];
+        const float counted = p.gate_kind == BIGMAC_GATE_CHANNEL ? dZ[i] : dn;
+        sum[AT_POST][i] = fmaf(counted, y[i], sum[AT_POST][i]);
+        if (BIAS) sum[AT_BIAS + (PRE ? 1 : 0)][i] += counted;
+        const float e = in_row * (dn * pw[i]);
+        dZ[i] = e;
+        q[0] += e;
+        q[1] = fmaf(e, y[i], q[1]);
       }
+      if (p.gate_kind == BIGMAC_GATE_FULL) store8(bdg, col, p.u_f32, dg);
       row_sums<W, 3, S::SLOTS>(q, box, turn, slot, wir, lane);
       if (p.gate_kind == BIGMAC_GATE_TOKEN && live && wir == 0 && lane == 0) ((float*)p.dgate)[row] = q[2];
       const float mean_e = p.layer ? q[0] * p.inv_d : 0.0f, c = q[1] * p.inv_d;
       const auto bdy = buffer(p.dy, p.u_f32);
+      float out[8];
 #pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        float out[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) out[i] = r * (dZ[v][i] - mean_e - y[v][i] * c);
-        store8(bdy, col[v], p.u_f32, out);
-      }
+      for (int i = 0; i < 8; ++i) out[i] = r * (dZ[i] - mean_e - y[i] * c);
+      store8(bdy, col, p.u_f32, out);
     }
   }
   // the workgroup's sums: the other slots' added to the first slot's in their order
 #pragma unroll
-  for (int k = 0; k < VECTORS; ++k)
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      float* f = sum[k][v];
-      if (S::SLOTS > 1) {
-        const int mine = wir * 64 + lane;
-        __syncthreads();
-        if (slot > 0) {
-          float4* to = join + ((slot - 1) * W * 64 + mine) * 2;
-          to[0] = make_float4(f[0], f[1], f[2], f[3]);
-          to[1] = make_float4(f[4], f[5], f[6], f[7]);
-        }
-        __syncthreads();
-        if (slot == 0)
-#pragma unroll
-          for (int o = 0; o < S::SLOTS - 1; ++o) {
-            const float4 a = join[(o * W * 64 + mine) * 2], c = join[(o * W * 64 + mine) * 2 + 1];
-            f[0] += a.x; f[1] += a.y; f[2] += a.z; f[3] += a.w;
-            f[4] += c.x; f[5] += c.y; f[6] += c.z; f[7] += c.w;
-          }
-      }
-      if (slot == 0 && col[v] < p.d) {
-        float4* to = (float4*)(p.part + ((size_t)blockIdx.x * VECTORS + k) * p.d + col[v]);
+  for (int k = 0; k < VECTORS; ++k) {
+    float* f = sum[k];
+    if (S::SLOTS > 1) {
+      const int mine = wir * 64 + lane;
+      __syncthreads();
+      if (slot > 0) {
+        float4* to = join + ((slot - 1) * W * 64 + mine) * 2;
         to[0] = make_float4(f[0], f[1], f[2], f[3]);
         to[1] = make_float4(f[4], f[5], f[6], f[7]);
       }
+      __syncthreads();
+      if (slot == 0)
+#pragma unroll
+        for (int o = 0; o < S::SLOTS - 1; ++o) {
+          const float4 a = join[(o * W * 64 + mine) * 2], c = join[(o * W * 64 + mine) * 2 + 1];
+          f[0] += a.x; f[1] += a.y; f[2] += a.z; f[3] += a.w;
+          f[4] += c.x; f[5] += c.y; f[6] += c.z; f[7] += c.w;
+        }
     }
+    if (slot == 0 && col < p.d) {
+      float4* to = (float4*)(p.part + ((size_t)blockIdx.x * VECTORS + k) * p.d + col);
+      to[0] = make_float4(f[0], f[1], f[2], f[3]);
+      to[1] = make_float4(f[4], f[5], f[6], f[7]);
+    }
+  }
 }
 
 // The workgroups' sums of a vector, 16 columns per workgroup: 64 groups of threads each add every 64th workgroup's, 4 columns a thread,
@@ -527,26 +471,26 @@ NormArgs norm_args(const bigmac_norm_dims& D, const bigmac_norm_params& P) {
   return a;
 }
 
-template <int W, int NV>
+template <int W>
 void forward_of(const NormArgs& a, bool post, bool pre, hipStream_t s) {
-  using S = RowShape<W, NV>;
+  using S = RowShape<W>;
   // a persistent grid of what the chip holds: eight workgroups of 256 threads a CU
   const int grid = std::min((a.T + S::SLOTS - 1) / S::SLOTS, 256 * 32 / S::WAVES);
-  if (post && pre) norm_forward_kernel<W, NV, true, true><<<grid, S::THREADS, 0, s>>>(a);
-  else if (post) norm_forward_kernel<W, NV, true, false><<<grid, S::THREADS, 0, s>>>(a);
-  else norm_forward_kernel<W, NV, false, true><<<grid, S::THREADS, 0, s>>>(a);
+  if (post && pre) norm_forward_kernel<W, true, true><<<grid, S::THREADS, 0, s>>>(a);
+  else if (post) norm_forward_kernel<W, true, false><<<grid, S::THREADS, 0, s>>>(a);
+  else norm_forward_kernel<W, false, true><<<grid, S::THREADS, 0, s>>>(a);
 }
-template <int W, int NV>
+template <int W>
 void backward_of(const NormArgs& a, bool post, bool pre, bool bias, int grid, hipStream_t s) {
-  constexpr int THREADS = RowShape<W, NV>::THREADS;
+  constexpr int THREADS = RowShape<W>::THREADS;
   if (bias) {
-    if (post && pre) norm_backward_kernel<W, NV, true, true, true><<<grid, THREADS, 0, s>>>(a);
-    else if (post) norm_backward_kernel<W, NV, true, false, true><<<grid, THREADS, 0, s>>>(a);
-    else norm_backward_kernel<W, NV, false, true, true><<<grid, THREADS, 0, s>>>(a);
+    if (post && pre) norm_backward_kernel<W, true, true, true><<<grid, THREADS, 0, s>>>(a);
+    else if (post) norm_backward_kernel<W, true, false, true><<<grid, THREADS, 0, s>>>(a);
+    else norm_backward_kernel<W, false, true, true><<<grid, THREADS, 0, s>>>(a);
   } else {
-    if (post && pre) norm_backward_kernel<W, NV, true, true, false><<<grid, THREADS, 0, s>>>(a);
-    else if (post) norm_backward_kernel<W, NV, true, false, false><<<grid, THREADS, 0, s>>>(a);
-    else norm_backward_kernel<W, NV, false, true, false><<<grid, THREADS, 0, s>>>(a);
+    if (post && pre) norm_backward_kernel<W, true, true, false><<<grid, THREADS, 0, s>>>(a);
+    else if (post) norm_backward_kernel<W, true, false, false><<<grid, THREADS, 0, s>>>(a);
+    else norm_backward_kernel<W, false, true, false><<<grid, THREADS, 0, s>>>(a);
   }
 }
 
@@ -575,11 +519,11 @@ int bigmac_norm_forward(const bigmac_norm_dims* D, const bigmac_norm_params* P, 
   a.x = x; a.y = y; a.z = z; a.u = u;
   hipStream_t s = (hipStream_t)stream;
   switch (waves_per_row(D->d)) {
-    case 1: forward_of<1, 1>(a, post, pre, s); break;
-    case 2: forward_of<2, 1>(a, post, pre, s); break;
-    case 4: forward_of<4, 1>(a, post, pre, s); break;
-    case 8: forward_of<8, 1>(a, post, pre, s); break;
-    default: forward_of<16, 1>(a, post, pre, s); break;
+    case 1: forward_of<1>(a, post, pre, s); break;
+    case 2: forward_of<2>(a, post, pre, s); break;
+    case 4: forward_of<4>(a, post, pre, s); break;
+    case 8: forward_of<8>(a, post, pre, s); break;
+    default: forward_of<16>(a, post, pre, s); break;
   }
   BIGMAC_CHECK_LAUNCH();
   return BIGMAC_OK;
@@ -605,11 +549,11 @@ int bigmac_norm_backward(const bigmac_norm_dims* D, const bigmac_norm_params* P,
   a.x = z; a.y = y; a.du = du; a.dz = dz; a.dx = dx; a.dy = dy; a.dgate = d_gate; a.part = (float*)ws;
   hipStream_t s = (hipStream_t)stream;
   switch (waves_per_row(D->d)) {
-    case 1: backward_of<1, 1>(a, post, pre, bias, workgroups, s); break;
-    case 2: backward_of<2, 1>(a, post, pre, bias, workgroups, s); break;
-    case 4: backward_of<4, 1>(a, post, pre, bias, workgroups, s); break;
-    case 8: backward_of<8, 1>(a, post, pre, bias, workgroups, s); break;
-    default: backward_of<16, 1>(a, post, pre, bias, workgroups, s); break;
+    case 1: backward_of<1>(a, post, pre, bias, workgroups, s); break;
+    case 2: backward_of<2>(a, post, pre, bias, workgroups, s); break;
+    case 4: backward_of<4>(a, post, pre, bias, workgroups, s); break;
+    case 8: backward_of<8>(a, post, pre, bias, workgroups, s); break;
+    default: backward_of<16>(a, post, pre, bias, workgroups, s); break;
   }
   BIGMAC_CHECK_LAUNCH();
   NormReduce r{};
