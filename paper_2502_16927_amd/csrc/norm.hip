@@ -241,7 +241,7 @@ __global__ __launch_bounds__((RowShape<W>::THREADS), BIAS ? 1 : 4) void norm_bac
     rdz.load(bdz, col, p.x_f32);
     if (POST && p.gate_kind == BIGMAC_GATE_FULL) rg.load(bg, col, p.u_f32);
     float token_gate = 1.0f;
-    if (POST && p.gate_kind == BIGMAC_GATE_TOKEN) token_gate = ((const float*)p.gate)[at];
+    if (POST && p.gate_kind == BIGMAC_GATE_TOKEN && live) token_gate = ((const float*)p.gate)[at];
 
     float z[8], du[8], y[8];
     if (PRE) {
@@ -287,6 +287,7 @@ __global__ __launch_bounds__((RowShape<W>::THREADS), BIAS ? 1 : 4) void norm_bac
           sum[AT_PRE][i] = fmaf(du[i], zh, sum[AT_PRE][i]);
           if (BIAS) sum[AT_BIAS][i] += du[i];
         }
+        if (!live) dZ[i] = 0.0f;   // (no row: adds nothing to the sums, whatever the weights hold)
         out[i] = p.alpha * dZ[i];
       }
       store8(bdx, col, p.x_f32, out);
