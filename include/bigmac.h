@@ -383,8 +383,8 @@ typedef struct {
 size_t bigmac_mx_workspace_bytes(const bigmac_mx_dims *dims); /* host only; 0 for bad dims */
 
 /* out[m, :] = A[m, :] W[e] (+ bias[e]) for the rows m of group e, offsets[e] <= m < offsets[e + 1] (device, [groups + 1], ascending from
- * 0, up to rows; rows at or past offsets[groups] are left as they were).  offsets == NULL: one group of all rows (groups = 1; ws
- * may be NULL).  A: codes and scales as bigmac_mx_quantize writes them; bias [groups, n_out] bf16 or NULL; out [rows, n_out]. */
+ * 0, up to rows; rows at or past offsets[groups] are left as they were).  Other offsets give unspecified results, but nothing outside
+ * the buffers is read or written.  offsets == NULL: one group of all rows (groups = 1; ws may be NULL).  A: codes and scales as bigmac_mx_quantize writes them; bias [groups, n_out] bf16 or NULL; out [rows, n_out]. */
 int bigmac_mx_product(const bigmac_mx_dims *dims, const void *codes, const void *scales, const int32_t *offsets, const void *packed,
                       const void *bias, void *out, void *ws, size_t ws_bytes, void *stream);
 

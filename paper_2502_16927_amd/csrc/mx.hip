@@ -29,26 +29,27 @@ __device__ __forceinline__ void put8(float* p, const float* f) {
 __device__ __forceinline__ void put8(bf16_t* p, const float* f) { *(uint4*)p = pack_bf16x8(f); }
 
 // The tile map by one workgroup of 256 threads, up to 1024 groups: tiles in front of every group (four groups a thread, a scan over the
-// wavefronts), then each thread finds the groups of every 256th tile.
+// wavefronts), then each thread finds the groups of every 256th tile.  Whatever the offsets hold, nothing is written past the map: counts wrap,
+// and the tiles are cut off at the most that ascending offsets make; the products leave out tiles outside their rows.
 __device__ __forceinline__ void build_mx_map(const MxMapJob& job) {
-  __shared__ int before[1025], wave_total[4];
+  __shared__ unsigned before[1025], wave_total[4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g0 = threadIdx.x * 4;
-  int count[4], sum = 0;
+  unsigned count[4], sum = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int g = g0 + i;
-    count[i] = g < job.groups ? (job.offsets[g + 1] - job.offsets[g] + job.tile_rows - 1) / job.tile_rows : 0;
+    count[i] = g < job.groups ? (unsigned)max((long)job.offsets[g + 1] - job.offsets[g] + job.tile_rows - 1, 0l) / (unsigned)job.tile_rows : 0;
     sum += count[i];
   }
-  int upto = sum;
+  unsigned upto = sum;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-    const int o = __shfl_up(upto, d, 64);
+    const unsigned o = __shfl_up(upto, d, 64);
     if (lane >= d) upto += o;
   }
   if (lane == 63) wave_total[wave] = upto;
   __syncthreads();
-  int at = upto - sum;
+  unsigned at = upto - sum;
   for (int w = 0; w < wave; ++w) at += wave_total[w];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -56,19 +57,19 @@ __device__ __forceinline__ void build_mx_map(const MxMapJob& job) {
     at += count[i];
   }
   if (threadIdx.x == 255) {
-    before[1024] = at;
-    job.map[0] = at;
+    before[1024] = min(at, (unsigned)mx_most_tiles(job.rows, job.groups, job.tile_rows));
+    job.map[0] = (int)before[1024];
   }
   __syncthreads();
-  const int tiles = before[1024];
-  for (int i = threadIdx.x; i < tiles; i += 256) {
+  const unsigned tiles = before[1024];
+  for (unsigned i = threadIdx.x; i < tiles; i += 256) {
     int lo = 0, hi = job.groups;           // the last group that starts at or in front of tile i: groups without rows start where the next one does
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
       if (before[mid] <= i) lo = mid;
       else hi = mid;
     }
-    *(int2*)(job.map + 2 + 2 * i) = make_int2(lo, job.offsets[lo] + (i - before[lo]) * job.tile_rows);
+    *(int2*)(job.map + 2 + 2 * i) = make_int2(lo, (int)((unsigned)job.offsets[lo] + (i - before[lo]) * (unsigned)job.tile_rows));
   }
 }
 __global__ __launch_bounds__(256) void mx_map_kernel(MxMapJob job) { build_mx_map(job); }
@@ -371,7 +372,7 @@ int bigmac_mx_product(const bigmac_mx_dims* D, const void* codes, const void* sc
   rc = check_mx_product(p);
   if (rc) return rc;
   if (offsets) {
-    mx_map_kernel<<<1, 256, 0, s>>>(MxMapJob{offsets, (int*)ws, D->groups, p.tile_rows});
+    mx_map_kernel<<<1, 256, 0, s>>>(MxMapJob{offsets, (int*)ws, D->rows, D->groups, p.tile_rows});
     BIGMAC_CHECK_LAUNCH();
   }
   return launch_mx_product(p, s);
@@ -392,7 +393,7 @@ int bigmac_mx_grouped_ffn(const bigmac_dims* D, const void* x_perm, const int32_
   hipStream_t s = (hipStream_t)stream;
   const int rows = (int)((long)D->T * D->k);
   uint8_t* base = (uint8_t*)ws;
-  const MxMapJob map{expert_offsets, (int*)(base + plan.map), D->N, mx_tile_rows(rows, D->N, std::min(W.win, W.hid))};
+  const MxMapJob map{expert_offsets, (int*)(base + plan.map), rows, D->N, mx_tile_rows(rows, D->N, std::min(W.win, W.hid))};
   MxProduct up{}, down{};
   up.codes = base + plan.x_codes; up.scales = base + plan.x_scales; up.packed = (const uint8_t*)w1; up.bias = (const bf16_t*)b1;
   up.out = base + plan.h_codes; up.out_scales = base + plan.h_scales;

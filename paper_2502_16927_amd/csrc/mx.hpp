@@ -72,8 +72,10 @@ int launch_mx_product(const MxProduct& p, hipStream_t s);
 struct MxMapJob {
   const int* offsets;              // device [groups + 1]
   int* map;                        // device, mx_map_ints(rows, groups); NULL: no job
-  int groups, tile_rows;
+  int rows, groups, tile_rows;
 };
+// upper bound of the row tiles (ascending offsets keep it by themselves, others are cut off at it)
+inline __host__ __device__ long mx_most_tiles(long rows, long groups, int tile_rows) { return rows / tile_rows + (groups < rows ? groups : rows); }
 inline size_t mx_map_ints(long rows, long groups) { return 2 + 2 * ((size_t)rows / 32 + groups + 1); }   // for every tile height
 // map (optional): the tile map by a workgroup of the same launch
 int launch_mx_quantize(long rows, long cols, int dtype, const void* src, uint8_t* codes, uint8_t* scales, hipStream_t s, const MxMapJob* map = nullptr);

@@ -84,7 +84,8 @@ __device__ __forceinline__ MxTile mx_part(const MxProduct& p, int parts) {
   if (p.offsets) {
     t.group = table_at(p.tile_map, 2 + 2 * tile);
     t.m0 = table_at(p.tile_map, 3 + 2 * tile);
-    m_end = table_at(p.offsets, t.group + 1);
+    m_end = min(table_at(p.offsets, t.group + 1), p.rows);
+    t.valid = t.m0 >= 0 && t.m0 < m_end;   // (offsets out of order or past the rows: nothing outside the buffers is touched)
   }
   t.m_rows = min(m_end - t.m0, BM);
   return t;
@@ -505,9 +506,8 @@ __global__ __launch_bounds__(256, 2) void mx_split_kernel(MxProduct p) {
   }
 }
 
-// upper bound of the row tiles
 long most_tiles(const MxProduct& p, int tile_rows) {
-  return p.offsets ? (long)p.rows / tile_rows + std::min(p.groups, p.rows) : ((long)p.rows + tile_rows - 1) / tile_rows;
+  return p.offsets ? mx_most_tiles(p.rows, p.groups, tile_rows) : ((long)p.rows + tile_rows - 1) / tile_rows;
 }
 // A quarter of the inputs per wavefront, for few tiles and a long walk: us without and with at 4096 inputs, 1024 columns: 1 row 8.4, 6.1;
 // 500 (64 tiles of 256 columns) 10.0, 8.3; 8 groups of 32 (32) 12.8, 10.9; 16 of 16 (64) 13.2, 12.3; 8 of 125 (128) 13.1, 15.6; at 1024 inputs within 0.4.

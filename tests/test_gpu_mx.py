@@ -216,6 +216,28 @@ def test_a_row_that_is_not_finite_stays_alone():
     assert torch.equal(got[keep], want[keep]) and torch.isnan(got[5]).all() and torch.isnan(got[60]).all()
 
 
+@pytest.mark.parametrize("rows", [70, 6000])
+@pytest.mark.parametrize("offsets", [lambda n: [0, 2 * n, 3 * n, 3 * n], lambda n: [0, n, 0, n], lambda n: [-n, 0, n, 2 * n], lambda n: [2 ** 31 - 1, -2 ** 31, 2 ** 31 - 1, 0],
+                                     lambda n: [n, n - 1, n - 2, 0]], ids=["past", "back", "negative", "extremes", "descending"])
+def test_offsets_that_are_not_offsets(rows, offsets):
+    """The product bounds every access by the rows and the map's size: what lies in front of and behind the buffers keeps its values."""
+    n_in, n_out, groups = 128, 320, 3
+    x = torch.ones((rows, n_in), dtype=torch.bfloat16, device=DEV)
+    _, _, codes, scales = quantised(x)
+    w = pack(torch.ones((groups, n_in, n_out), dtype=torch.bfloat16, device=DEV))
+    dims = B.make_mx_dims(rows, groups, n_in, n_out, B.F32)
+    size = B.mx_workspace_bytes(dims)
+    ws = torch.full((size + 8192,), 0xEE, dtype=torch.uint8, device=DEV)
+    out = torch.full((rows + 512, n_out), 7.0, device=DEV)
+    at = torch.tensor(offsets(rows), dtype=torch.int64).to(torch.int32).to(DEV)
+    print(f"offsets {offsets(rows)}, {rows} rows", flush=True)
+    B.bigmac_mx_product(dims, codes, scales, at, w, None, out[256:256 + rows], ws[4096:4096 + size])
+    assert (out[:256] == 7.0).all() and (out[256 + rows:] == 7.0).all(), "beside the rows"
+    assert (ws[:4096] == 0xEE).all() and (ws[4096 + size:] == 0xEE).all(), "beside the workspace"
+    inside = out[256:256 + rows]
+    assert ((inside == 7.0) | (inside == n_in)).all()
+
+
 # ------------------------------------------------------------------ the experts' FFN
 
 class Ffn:
