@@ -362,9 +362,9 @@ int bigmac_norm_backward(const bigmac_norm_dims *dims, const bigmac_norm_params 
  * Base pointers 16-byte aligned (BIGMAC_ERR_INVALID_ARG else).  Past 1024 groups, 2^30 rows, 2^24 columns, or 2^24 workgroups in a
  * launch: BIGMAC_ERR_TOO_LARGE. */
 
-/* Rows (operands of a product on the left): codes [rows, cols / 2], value 2i in the low half of byte i; scales [rows,
- * bigmac_mx_scale_bytes(cols)]: 8 bytes per 256 columns, block b of them at byte (b % 2) * 4 + b / 2, unused bytes 0.  cols a multiple
- * of 32.  Host only; 0 for a bad cols. */
+/* Rows (operands of a product on the left): codes [rows, cols / 2], value 2i in the low half of byte i; scales [cols / 256,
+ * rounded up][rows][8]: of 256 columns' blocks, block b at byte (b % 2) * 4 + b / 2, unused bytes 0 (rows: of the call that quantises and of
+ * the product that reads them).  bigmac_mx_scale_bytes: bytes per row.  cols a multiple of 32.  Host only; 0 for a bad cols. */
 size_t bigmac_mx_scale_bytes(int64_t cols);
 int bigmac_mx_quantize(int64_t rows, int64_t cols, int32_t dtype, const void *src /*[rows,cols] dtype*/, void *codes, void *scales, void *stream);
 int bigmac_mx_dequantize(int64_t rows, int64_t cols, const void *codes, const void *scales, int32_t dtype, void *dst /*[rows,cols]*/, void *stream);

@@ -91,7 +91,7 @@ __global__ __launch_bounds__(256) void mx_quantize_kernel(const T* __restrict__ 
     for (int j = 0; j < ROW_TURNS; ++j) {
       const long row = ((long)blockIdx.x * ROW_TURNS + j) * rows_at_once + ty;
       if (row >= rows) break;
-      uint8_t* to = scales + row * scale_bytes + mx_scale_at((unsigned)p / 4);
+      uint8_t* to = scales + mx_scale_at(rows, row, (unsigned)p / 4);
       if (p >= pieces) {
         if ((p & 3) == 0) *to = 0;
         continue;
@@ -112,7 +112,7 @@ __global__ __launch_bounds__(256) void mx_quantize_kernel(const T* __restrict__ 
 
 template <typename T>
 __global__ __launch_bounds__(256) void mx_dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, T* __restrict__ dst, long rows,
-                                                            int cols, int log_tx, int scale_bytes) {
+                                                            int cols, int log_tx) {
   const int tx = threadIdx.x & ((1 << log_tx) - 1), ty = threadIdx.x >> log_tx, rows_at_once = 256 >> log_tx;
   const int pieces = cols / 8;
   for (int p = tx; p < pieces; p += 1 << log_tx) {
@@ -121,7 +121,7 @@ __global__ __launch_bounds__(256) void mx_dequantize_kernel(const uint8_t* __res
       const long row = ((long)blockIdx.x * ROW_TURNS + j) * rows_at_once + ty;
       if (row >= rows) break;
       float f[8];
-      mx_values8(*(const unsigned*)(codes + row * (cols / 2) + (long)p * 4), mx_scale(scales[row * scale_bytes + mx_scale_at((unsigned)p / 4)]), f);
+      mx_values8(*(const unsigned*)(codes + row * (cols / 2) + (long)p * 4), mx_scale(scales[mx_scale_at(rows, row, (unsigned)p / 4)]), f);
       put8(dst + row * cols + (long)p * 8, f);
     }
   }
@@ -315,11 +315,10 @@ int bigmac_mx_dequantize(int64_t rows, int64_t cols, const void* codes, const vo
   const int rc = check_rows(rows, cols, dtype);
   if (rc) return rc;
   if (!dst || !codes || !scales || !aligned({dst, codes, scales})) return BIGMAC_ERR_INVALID_ARG;
-  const int scale_bytes = (int)mx_scale_bytes(cols);
   const RowGrid g = row_grid(rows, cols / 8);
   hipStream_t s = (hipStream_t)stream;
-  if (dtype == BIGMAC_BF16) mx_dequantize_kernel<bf16_t><<<(unsigned)g.blocks, 256, 0, s>>>((const uint8_t*)codes, (const uint8_t*)scales, (bf16_t*)dst, rows, (int)cols, g.log_tx, scale_bytes);
-  else mx_dequantize_kernel<float><<<(unsigned)g.blocks, 256, 0, s>>>((const uint8_t*)codes, (const uint8_t*)scales, (float*)dst, rows, (int)cols, g.log_tx, scale_bytes);
+  if (dtype == BIGMAC_BF16) mx_dequantize_kernel<bf16_t><<<(unsigned)g.blocks, 256, 0, s>>>((const uint8_t*)codes, (const uint8_t*)scales, (bf16_t*)dst, rows, (int)cols, g.log_tx);
+  else mx_dequantize_kernel<float><<<(unsigned)g.blocks, 256, 0, s>>>((const uint8_t*)codes, (const uint8_t*)scales, (float*)dst, rows, (int)cols, g.log_tx);
   BIGMAC_CHECK_LAUNCH();
   return BIGMAC_OK;
 }

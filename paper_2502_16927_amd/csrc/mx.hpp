@@ -7,11 +7,12 @@ namespace bigmac {
 
 constexpr int MX_BLOCK = 32, MX_STEP = 64, MX_CHUNK = 256;   // values: per scale, per matrix instruction, per dword of four scales of a lane
 
-// Rows: codes [rows][cols / 2], value 2i in the low half of byte i; scales [rows][mx_scale_bytes(cols)], 8 bytes per 256 columns of which
-// the first four belong to the even blocks and the other four to the odd ones, unused bytes 0.  A lane of a matrix instruction holds
-// the even or the odd block of a row and reads the scales of four instructions as one dword.
+// Rows: codes [rows][cols / 2], value 2i in the low half of byte i; scales [cols / 256, rounded up][rows][8]: of 8 bytes the first four
+// belong to the even blocks and the other four to the odd ones, unused bytes 0.  A lane of a matrix instruction holds the even or the odd
+// block of a row and reads the scales of four instructions as one dword; the scales that a tile's rows need at a time are whole lines.
+// (A row's scales one after another cost a line per row: 16 KB of lines beside the 48 KB of operands of 128 rows x 256 columns.)
 inline size_t mx_scale_bytes(long cols) { return (size_t)((cols + MX_CHUNK - 1) / MX_CHUNK) * 8; }
-__device__ __forceinline__ unsigned mx_scale_at(unsigned block) { return (block & ~7u) + (block & 1) * 4 + ((block & 7) >> 1); }
+__device__ __forceinline__ size_t mx_scale_at(long rows, long row, unsigned block) { return ((size_t)(block >> 3) * rows + row) * 8 + (block & 1) * 4 + ((block & 7) >> 1); }
 
 // Weights: 32 output columns x 64 inputs are the 1 KB that a wavefront feeds to one matrix instruction, lane l's 16 bytes (column l % 32,
 // inputs 32 (l / 32) .. + 31) one after another.  A strip of 32 columns: [n_in / 64][64 lanes][16] codes, behind them its scales,
@@ -55,7 +56,7 @@ constexpr long MX_MAX_BLOCKS = 0xFFFFFF;   // of 256 threads: a launch has under
 enum MxEpilogue { MX_STORE_BF16 = 0, MX_STORE_F32 = 1, MX_GELU_CODES = 2 };
 // C = A W[group] (+ bias[group]) over ragged or dense rows
 struct MxProduct {
-  const uint8_t *codes, *scales;   // A: [rows][n_in]
+  const uint8_t *codes, *scales;   // A: rows x n_in
   const uint8_t* packed;           // W: [groups] of n_in x n_out
   const bf16_t* bias;              // [groups][n_out] or NULL
   const int* offsets;              // device [groups + 1], or NULL: one group of all rows

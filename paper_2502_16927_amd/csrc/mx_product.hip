@@ -202,6 +202,10 @@ __device__ __forceinline__ void mx_bias(const MxProduct& p, const MxTile& t, int
 // 256 x 256 tiles by eight wavefronts (960 against 819), 64-row tiles (885 against 797), 32 columns a wavefront (888 against 874), weights two
 // chunks ahead (807 against 796), the rows of a tile kept in the LDS for all columns (803 against 799).
 constexpr int MX_STAGES = 3;
+// the scales of a tile's rows for the 256 inputs of a chunk
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t chunk_scales(const MxProduct& p, const MxTile& t, int chunk) {
+  return scalar_buffer((size_t)p.scales + ((size_t)chunk * p.rows + t.m0) * 8, (size_t)t.m_rows * 8);
+}
 constexpr unsigned mx_stage_bytes(int mt) { return mt * 4096 + 1024; }   // codes; 256 dwords of scales (past the tile's rows: zeros)
 template <int MT, int NS, int EPI>
 __device__ __forceinline__ void mx_tile_product(const MxProduct& p, const MxTile& t, uint4* ring, uint4* staging, uint8_t* out_scales) {
@@ -211,9 +215,8 @@ __device__ __forceinline__ void mx_tile_product(const MxProduct& p, const MxTile
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int strips = p.n_out / 32, strip0 = t.strip0 + wave * NS;
   const int steps = p.n_in / MX_STEP, chunks = (steps + 3) / 4;
-  const unsigned row_bytes = (unsigned)p.n_in / 2, scale_bytes = (unsigned)chunks * 8;
+  const unsigned row_bytes = (unsigned)p.n_in / 2;
   const auto ba = scalar_buffer((size_t)p.codes + (size_t)t.m0 * row_bytes, (size_t)t.m_rows * row_bytes);
-  const auto bs = scalar_buffer((size_t)p.scales + (size_t)t.m0 * scale_bytes, (size_t)t.m_rows * scale_bytes);
   const unsigned strip_bytes = (unsigned)mx_strip_bytes(p.n_in), scales_at = (unsigned)steps * 1024u;   // of a strip of the weights
   __amdgpu_buffer_rsrc_t bw[NS];
 #pragma unroll
@@ -227,7 +230,6 @@ __device__ __forceinline__ void mx_tile_product(const MxProduct& p, const MxTile
   constexpr int DMA = MT;                   // 16-byte requests of a lane per chunk, 32 rows each
   const unsigned swizzle = (threadIdx.x >> 4) & 7;
   const unsigned a_off = (threadIdx.x >> 3) * row_bytes + ((threadIdx.x & 7) ^ swizzle) * 16u, a_pass = 32u * row_bytes;
-  const unsigned s_off = (threadIdx.x >> 1) * scale_bytes + (threadIdx.x & 1) * 4u;
   // Past the last chunk: out of range, zeros that nobody reads.  (Requested all the same: with a branch in the loop the compiler moves
   // the matrix instructions in front of it, which it takes for arithmetic like any other, behind it, and keeps their operands.)
   auto request = [&](int chunk, unsigned stage) {
@@ -237,8 +239,8 @@ __device__ __forceinline__ void mx_tile_product(const MxProduct& p, const MxTile
     for (int i = 0; i < DMA; ++i)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(ba, (__attribute__((address_space(3))) void*)(ring + stage / 16 + i * 256 + wave * 64), 16,
                                                (a_off + i * a_pass + (unsigned)chunk * 128u) | at, 0, 0, 0);
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(bs, (__attribute__((address_space(3))) void*)(ring + stage / 16 + CODES / 16 + wave * 16), 4,
-                                             (s_off + (unsigned)chunk * 8u) | at, 0, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(chunk_scales(p, t, chunk), (__attribute__((address_space(3))) void*)(ring + stage / 16 + CODES / 16 + wave * 16), 4,
+                                             (threadIdx.x * 4u) | at, 0, 0, 0);
 #endif
     asm volatile("" ::: "memory");
   };
@@ -381,7 +383,7 @@ __device__ __forceinline__ void mx_tile_product(const MxProduct& p, const MxTile
         }
     }
     __syncthreads();
-    const size_t row_out = (size_t)p.n_out / 2, scales_out = (size_t)((p.n_out + MX_CHUNK - 1) / MX_CHUNK) * 8;
+    const size_t row_out = (size_t)p.n_out / 2;
     const int pieces = min(8, strips - t.strip0);   // of the workgroup's 256 columns, 32 each
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
@@ -391,7 +393,7 @@ __device__ __forceinline__ void mx_tile_product(const MxProduct& p, const MxTile
     }
     // (bytes of blocks past the last column are whatever the LDS held: nobody reads them)
     if ((int)threadIdx.x < t.m_rows)
-      *(uint2*)(p.out_scales + (size_t)(t.m0 + (int)threadIdx.x) * scales_out + t.strip0) = *(const uint2*)(out_scales + threadIdx.x * 8);
+      *(uint2*)(p.out_scales + mx_scale_at(p.rows, t.m0 + (int)threadIdx.x, t.strip0)) = *(const uint2*)(out_scales + threadIdx.x * 8);
   } else {
     if (!there) return;
 #pragma unroll
@@ -429,14 +431,13 @@ __global__ __launch_bounds__(256, 2) void mx_split_kernel(MxProduct p) {
   const MxTile t = mx_tile<32, NS>(p);
   if (!t.valid) return;
   const int strips = p.n_out / 32, steps = p.n_in / MX_STEP, chunks = (steps + 3) / 4;
-  const unsigned row_bytes = (unsigned)p.n_in / 2, scale_bytes = (unsigned)chunks * 8;
+  const unsigned row_bytes = (unsigned)p.n_in / 2;
   const auto ba = scalar_buffer((size_t)p.codes + (size_t)t.m0 * row_bytes, (size_t)t.m_rows * row_bytes);
-  const auto bs = scalar_buffer((size_t)p.scales + (size_t)t.m0 * scale_bytes, (size_t)t.m_rows * scale_bytes);
   const unsigned strip_bytes = (unsigned)mx_strip_bytes(p.n_in), scales_at = (unsigned)steps * 1024u;   // of a strip of the weights
   __amdgpu_buffer_rsrc_t bw[NS];
 #pragma unroll
   for (int j = 0; j < NS; ++j) bw[j] = scalar_buffer((size_t)p.packed + ((size_t)t.group * strips + t.strip0 + j) * strip_bytes, strip_bytes);
-  const unsigned a_off = (unsigned)(lane & 31) * row_bytes + ((unsigned)lane >> 5) * 16u, s_off = (unsigned)(lane & 31) * scale_bytes + ((unsigned)lane >> 5) * 4u;
+  const unsigned a_off = (unsigned)(lane & 31) * row_bytes + ((unsigned)lane >> 5) * 16u, s_off = (unsigned)(lane & 31) * 8u + ((unsigned)lane >> 5) * 4u;
   struct Chunk {
     u32x4_t w[NS][4], a[4];
     unsigned ws[NS], as;
@@ -450,7 +451,7 @@ __global__ __launch_bounds__(256, 2) void mx_split_kernel(MxProduct p) {
       for (int ks = 0; ks < 4; ++ks)
         c.w[j][ks] = __builtin_amdgcn_raw_buffer_load_b128(bw[j], chunk * 4 + ks < steps ? (unsigned)(chunk * 4 + ks) * 1024u + lane * 16u : 0x80000000u, 0, 0);
     }
-    c.as = __builtin_amdgcn_raw_buffer_load_b32(bs, s_off + (unsigned)chunk * 8u, 0, 0);
+    c.as = __builtin_amdgcn_raw_buffer_load_b32(chunk_scales(p, t, chunk), s_off, 0, 0);
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) c.a[ks] = __builtin_amdgcn_raw_buffer_load_b128(ba, a_off + (unsigned)chunk * 128u + ks * 32u, 0, 0);
   };
@@ -499,7 +500,7 @@ __global__ __launch_bounds__(256, 2) void mx_split_kernel(MxProduct p) {
     const int row = lane & 31, strip = t.strip0 + (lane >> 5);
     if (row < t.m_rows) {
       *(uint4*)((uint8_t*)p.out + (size_t)(t.m0 + row) * (p.n_out / 2) + (size_t)strip * 16) = block;
-      p.out_scales[(size_t)(t.m0 + row) * ((p.n_out + MX_CHUNK - 1) / MX_CHUNK * 8) + mx_scale_at(strip)] = (uint8_t)(lane < 32 ? bytes[0] : bytes[1]);
+      p.out_scales[mx_scale_at(p.rows, t.m0 + row, strip)] = (uint8_t)(lane < 32 ? bytes[0] : bytes[1]);
     }
   } else {
     mx_store<NS>(p, acc, bias, t.m0, t.m_rows, t.strip0 * 32, (char*)staging, lane, std::integral_constant<int, EPI>{});

@@ -31,9 +31,9 @@ def quantised(src):
     """Codes and scales of the library, as numpy: codes [rows, cols], scale bytes in block order, and the buffers."""
     rows, cols = src.shape
     codes = torch.full((rows, cols // 2), 0xEE, dtype=torch.uint8, device=DEV)
-    scales = torch.full((rows, B.mx_scale_bytes(cols)), 0xEE, dtype=torch.uint8, device=DEV)
+    scales = torch.full((B.mx_scale_bytes(cols) // 8, rows, 8), 0xEE, dtype=torch.uint8, device=DEV)
     B.bigmac_mx_quantize(rows, cols, B.BF16 if src.dtype == torch.bfloat16 else B.F32, src, codes, scales)
-    c, s = codes.cpu().numpy().astype(np.int64), scales.cpu().numpy().astype(np.int64)
+    c, s = codes.cpu().numpy().astype(np.int64), scales.cpu().numpy().astype(np.int64).transpose(1, 0, 2).reshape(rows, -1)
     used = scale_place(cols // 32)
     assert (np.delete(s, used, 1) == 0).all(), "unused scale bytes"
     return np.stack([c & 15, c >> 4], 2).reshape(rows, cols), s[:, used], codes, scales
