@@ -79,9 +79,10 @@ constexpr int ROW_TURNS = 4;   // rows a thread takes
 // 1 << log_tx threads side by side on a row, the others on further rows
 template <typename T>
 __global__ __launch_bounds__(256) void mx_quantize_kernel(const T* __restrict__ src, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales, long rows,
-                                                          int cols, int log_tx, int scale_bytes, MxMapJob map) {
-  if (map.map && blockIdx.x == gridDim.x - 1) {
-    build_mx_map(map);
+                                                          int cols, int log_tx, int scale_bytes, MxMapJob map0, MxMapJob map1) {
+  if (map0.map && blockIdx.x >= gridDim.x - (map1.map ? 2 : 1)) {
+    if (blockIdx.x == gridDim.x - 1) build_mx_map(map0);
+    else build_mx_map(map1);
     return;
   }
   const int tx = threadIdx.x & ((1 << log_tx) - 1), ty = threadIdx.x >> log_tx, rows_at_once = 256 >> log_tx;
@@ -247,7 +248,7 @@ bool aligned(std::initializer_list<const void*> ps) {
 constexpr long MAX_ROWS = 1l << 30, MAX_COLS = 1l << 24;
 int check_rows(int64_t rows, int64_t cols, int dtype) {
   if (rows < 1 || cols < 32 || cols % 32 || (dtype != BIGMAC_F32 && dtype != BIGMAC_BF16)) return BIGMAC_ERR_INVALID_ARG;
-  return rows > MAX_ROWS || cols > MAX_COLS || row_grid(rows, cols / 8).blocks >= MX_MAX_BLOCKS ? BIGMAC_ERR_TOO_LARGE : BIGMAC_OK;
+  return rows > MAX_ROWS || cols > MAX_COLS || row_grid(rows, cols / 8).blocks >= MX_MAX_BLOCKS - 1 ? BIGMAC_ERR_TOO_LARGE : BIGMAC_OK;
 }
 long pack_blocks(long groups, long n_in, long n_out) { return (groups * ((n_in + MX_CHUNK - 1) / MX_CHUNK) * 2 * (n_out / 4) + 255) / 256; }
 int check_weights(int32_t groups, int32_t n_in, int32_t n_out) {
@@ -262,7 +263,7 @@ int check_mx(const bigmac_mx_dims* D) {
 size_t mx_map_bytes(int rows, int groups) { return align_up(mx_map_ints(rows, groups) * 4); }
 
 struct FfnPlan {
-  size_t x_codes, x_scales, h_codes, h_scales, map, total;
+  size_t x_codes, x_scales, h_codes, h_scales, up_map, down_map, total;
 };
 FfnPlan plan_ffn(const bigmac_dims& D) {
   const Widths W = widths(D);
@@ -272,20 +273,21 @@ FfnPlan plan_ffn(const bigmac_dims& D) {
   p.x_scales = align_up(rows * W.win / 2);
   p.h_codes = p.x_scales + align_up(rows * mx_scale_bytes(W.win));
   p.h_scales = p.h_codes + align_up(rows * W.hid / 2);
-  p.map = p.h_scales + align_up(rows * mx_scale_bytes(W.hid));
-  p.total = p.map + mx_map_bytes((int)rows, D.N);
+  p.up_map = p.h_scales + align_up(rows * mx_scale_bytes(W.hid));
+  p.down_map = p.up_map + mx_map_bytes((int)rows, D.N);
+  p.total = p.down_map + mx_map_bytes((int)rows, D.N);
   return p;
 }
 
 }  // namespace
 
-int launch_mx_quantize(long rows, long cols, int dtype, const void* src, uint8_t* codes, uint8_t* scales, hipStream_t s, const MxMapJob* map) {
+int launch_mx_quantize(long rows, long cols, int dtype, const void* src, uint8_t* codes, uint8_t* scales, hipStream_t s, const MxMapJob* maps) {
   const int scale_bytes = (int)mx_scale_bytes(cols);
   const RowGrid g = row_grid(rows, cols / 8);
-  const MxMapJob job = map ? *map : MxMapJob{};
-  const unsigned blocks = (unsigned)g.blocks + (map ? 1 : 0);
-  if (dtype == BIGMAC_BF16) mx_quantize_kernel<bf16_t><<<blocks, 256, 0, s>>>((const bf16_t*)src, codes, scales, rows, (int)cols, g.log_tx, scale_bytes, job);
-  else mx_quantize_kernel<float><<<blocks, 256, 0, s>>>((const float*)src, codes, scales, rows, (int)cols, g.log_tx, scale_bytes, job);
+  const MxMapJob map0 = maps ? maps[0] : MxMapJob{}, map1 = maps ? maps[1] : MxMapJob{};
+  const unsigned blocks = (unsigned)g.blocks + (map0.map ? 1 : 0) + (map1.map ? 1 : 0);
+  if (dtype == BIGMAC_BF16) mx_quantize_kernel<bf16_t><<<blocks, 256, 0, s>>>((const bf16_t*)src, codes, scales, rows, (int)cols, g.log_tx, scale_bytes, map0, map1);
+  else mx_quantize_kernel<float><<<blocks, 256, 0, s>>>((const float*)src, codes, scales, rows, (int)cols, g.log_tx, scale_bytes, map0, map1);
   BIGMAC_CHECK_LAUNCH();
   return BIGMAC_OK;
 }
@@ -361,7 +363,7 @@ int bigmac_mx_product(const bigmac_mx_dims* D, const void* codes, const void* sc
   p.out = out;
   p.rows = D->rows; p.groups = D->groups; p.n_in = D->n_in; p.n_out = D->n_out;
   p.epilogue = D->out_dtype == BIGMAC_F32 ? MX_STORE_F32 : MX_STORE_BF16;
-  p.tile_rows = mx_tile_rows(D->rows, D->groups, D->n_out);
+  p.tile_rows = mx_tile_rows(D->rows, D->groups, D->n_in, D->n_out, p.epilogue);
   if (offsets) {
     if (!ws || !aligned({ws})) return BIGMAC_ERR_INVALID_ARG;
     if (ws_bytes < mx_map_bytes(D->rows, D->groups)) return BIGMAC_ERR_WORKSPACE;
@@ -392,7 +394,6 @@ int bigmac_mx_grouped_ffn(const bigmac_dims* D, const void* x_perm, const int32_
   hipStream_t s = (hipStream_t)stream;
   const int rows = (int)((long)D->T * D->k);
   uint8_t* base = (uint8_t*)ws;
-  const MxMapJob map{expert_offsets, (int*)(base + plan.map), rows, D->N, mx_tile_rows(rows, D->N, std::min(W.win, W.hid))};
   MxProduct up{}, down{};
   up.codes = base + plan.x_codes; up.scales = base + plan.x_scales; up.packed = (const uint8_t*)w1; up.bias = (const bf16_t*)b1;
   up.out = base + plan.h_codes; up.out_scales = base + plan.h_scales;
@@ -400,13 +401,19 @@ int bigmac_mx_grouped_ffn(const bigmac_dims* D, const void* x_perm, const int32_
   down.codes = base + plan.h_codes; down.scales = base + plan.h_scales; down.packed = (const uint8_t*)w2; down.bias = (const bf16_t*)b2;
   down.out = o_perm;
   down.n_in = W.hid; down.n_out = W.win; down.epilogue = MX_STORE_BF16;
+  up.tile_rows = mx_tile_rows(rows, D->N, up.n_in, up.n_out, up.epilogue);
+  down.tile_rows = mx_tile_rows(rows, D->N, down.n_in, down.n_out, down.epilogue);
+  MxMapJob maps[2] = {{expert_offsets, (int*)(base + plan.up_map), rows, D->N, up.tile_rows}, {}};
+  if (down.tile_rows != up.tile_rows) maps[1] = {expert_offsets, (int*)(base + plan.down_map), rows, D->N, down.tile_rows};
+  up.tile_map = maps[0].map;
+  down.tile_map = maps[1].map ? maps[1].map : maps[0].map;
   for (MxProduct* p : {&up, &down}) {
-    p->offsets = expert_offsets; p->tile_map = map.map; p->tile_rows = map.tile_rows;
+    p->offsets = expert_offsets;
     p->rows = rows; p->groups = D->N;
     rc = check_mx_product(*p);
     if (rc) return rc;
   }
-  rc = launch_mx_quantize(rows, W.win, BIGMAC_BF16, x_perm, base + plan.x_codes, base + plan.x_scales, s, &map);
+  rc = launch_mx_quantize(rows, W.win, BIGMAC_BF16, x_perm, base + plan.x_codes, base + plan.x_scales, s, maps);
   if (!rc) rc = launch_mx_product(up, s);
   return rc ? rc : launch_mx_product(down, s);
 }

@@ -104,18 +104,18 @@ __device__ __forceinline__ unsigned piece_place(unsigned row, unsigned piece) { 
 // Results leave as whole lines.  A sub-tile of 32 x 32 lies in the lanes as: row l % 32, columns 8 q + 4 (l / 32) + 0 .. 3 in values 4 q .. 4 q + 3.
 // bf16 and fp32: through 4 KB of the wavefront's own, 32 rows x 128 bytes.  (Stored from where they lie, 32 bytes of a row at a time, they
 // were four requests a line; the 8 and 1 bytes of the 4-bit epilogue 16 and 8.)
+template <int PIECES = 8>   // of 16 bytes: a line, or half of one
 __device__ __forceinline__ void strip_out(char* strip, const MxProduct& p, int row0, int rows, size_t col_byte, size_t row_bytes, int lane) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const unsigned q = i * 64 + lane, row = q >> 3;
-    const uint4 v = *(const uint4*)(strip + piece_place(row, q & 7));
-    if ((int)row < rows) *(uint4*)((char*)p.out + (size_t)(row0 + (int)row) * row_bytes + col_byte + (q & 7) * 16) = v;
+  for (int i = 0; i < PIECES / 2; ++i) {
+    const unsigned q = i * 64 + lane, row = q / PIECES, piece = q % PIECES;
+    const uint4 v = *(const uint4*)(strip + piece_place(row, piece));
+    if ((int)row < rows) *(uint4*)((char*)p.out + (size_t)(row0 + (int)row) * row_bytes + col_byte + piece * 16) = v;
   }
 }
 template <int NS>
 __device__ __forceinline__ void mx_store(const MxProduct& p, const f32x16_t (&acc)[NS], const float (&bias)[NS][16], int row0, int rows, int col0, char* strip, int lane,
                                          std::integral_constant<int, MX_STORE_BF16>) {
-  static_assert(NS == 2, "64 columns are a line of bf16");
   const int half = lane >> 5;
 #pragma unroll
   for (int j = 0; j < NS; ++j)
@@ -129,7 +129,7 @@ __device__ __forceinline__ void mx_store(const MxProduct& p, const f32x16_t (&ac
       const auto r1 = __builtin_amdgcn_permlane32_swap(f2bf_pair(f[2], f[3]), f2bf_pair(f[6], f[7]), false, false);
       *(uint4*)(strip + piece_place(lane & 31, j * 4 + s * 2 + half)) = make_uint4(r0[0], r1[0], r0[1], r1[1]);
     }
-  strip_out(strip, p, row0, rows, (size_t)col0 * 2, (size_t)p.n_out * 2, lane);
+  strip_out<4 * NS>(strip, p, row0, rows, (size_t)col0 * 2, (size_t)p.n_out * 2, lane);
 }
 template <int NS>
 __device__ __forceinline__ void mx_store(const MxProduct& p, const f32x16_t (&acc)[NS], const float (&bias)[NS][16], int row0, int rows, int col0, char* strip, int lane,
@@ -188,7 +188,7 @@ __device__ __forceinline__ void mx_bias(const MxProduct& p, const MxTile& t, int
     }
 }
 
-// MT x 32 rows, 4 wavefronts side by side with NS x 32 columns each.
+// MT x 32 rows, 4 wavefronts side by side with NS x 32 columns each (NS 1: 64 rows without the GELU epilogue).
 //
 // Weights go from memory to registers as they lie there (1 KB per instruction operand, whole lines), each wavefront its own columns'.
 // Rows go straight to the LDS in chunks of 256 inputs, three stages: while chunk c is multiplied, chunk c + 1 has landed or is about
@@ -200,7 +200,8 @@ __device__ __forceinline__ void mx_bias(const MxProduct& p, const MxTile& t, int
 // 1.8 GHz), without its LDS reads too 160: power holds the clock down, and the requests cost as much as the epilogue.  Two workgroups share a CU.
 // Slower or level: one persistent workgroup walking many tiles with its operands requested a tile ahead (917 us a 16384-token call against 873),
 // 256 x 256 tiles by eight wavefronts (960 against 819), 64-row tiles (885 against 797), 32 columns a wavefront (888 against 874), weights two
-// chunks ahead (807 against 796), the rows of a tile kept in the LDS for all columns (803 against 799).
+// chunks ahead (807 against 796), the rows of a tile kept in the LDS for all columns (803 against 799); for 32-row tiles weights two chunks ahead
+// and eight wavefronts with half of the inputs each (+0.2 and +0.6 us at 512 -> 1024 to 4096 -> 4096: their CU is bound by what it takes in).
 constexpr int MX_STAGES = 3;
 // the scales of a tile's rows for the 256 inputs of a chunk
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t chunk_scales(const MxProduct& p, const MxTile& t, int chunk) {
@@ -404,15 +405,17 @@ __device__ __forceinline__ void mx_tile_product(const MxProduct& p, const MxTile
 }
 
 template <int MT, int NS, int EPI>
-__global__ __launch_bounds__(256, MT == 4 ? 2 : 4) void mx_product_kernel(MxProduct p) {
+__global__ __launch_bounds__(256, MT == 4 ? 2 : MT == 2 ? 3 : 4) void mx_product_kernel(MxProduct p) {
   constexpr int BM = MT * 32;
   __shared__ uint4 ring[MX_STAGES * mx_stage_bytes(MT) / 16];
   __shared__ uint4 staging[(EPI == MX_GELU_CODES ? BM * 128 : 4 * 4096) / 16];
   __shared__ __align__(16) uint8_t out_scales[EPI == MX_GELU_CODES ? BM * 8 : 8];
   const MxTile t = mx_tile<BM, 4 * NS>(p);
   if (!t.valid) return;
-  if constexpr (MT == 4) {   // the last rows of a group
+  if constexpr (MT > 1) {   // the last rows of a group
     if (t.m_rows <= 32) return mx_tile_product<1, NS, EPI>(p, t, ring, staging, out_scales);
+  }
+  if constexpr (MT == 4) {
     if (t.m_rows <= 64) return mx_tile_product<2, NS, EPI>(p, t, ring, staging, out_scales);
     if (t.m_rows <= 96) return mx_tile_product<3, NS, EPI>(p, t, ring, staging, out_scales);
   }
@@ -516,9 +519,10 @@ long even_tiles(long rows, long groups, int tile_rows) {   // rows spread evenly
   const long busy = std::min(rows, groups), each = (rows + busy - 1) / busy;
   return busy * ((each + tile_rows - 1) / tile_rows);
 }
-bool splits(const MxProduct& p) { return p.tile_rows == 32 && p.n_in >= 2048 && even_tiles(p.rows, p.groups, 32) * ((p.n_out + 255) / 256) <= 64; }
+bool worth_splitting(long rows, long groups, int n_in, int n_out) { return n_in >= 2048 && even_tiles(rows, groups, 32) * ((n_out + 255) / 256) <= 64; }
+bool splits(const MxProduct& p) { return p.tile_rows == 32 && worth_splitting(p.rows, p.groups, p.n_in, p.n_out); }
 long product_blocks(const MxProduct& p) {
-  const int columns = splits(p) ? 64 : 256;
+  const int columns = splits(p) ? 64 : p.tile_rows == 64 && p.epilogue != MX_GELU_CODES ? 128 : 256;
   return (most_tiles(p, p.tile_rows) * ((p.n_out + columns - 1) / columns) + 7) / 8 * 8;
 }
 template <int MT>
@@ -526,6 +530,11 @@ void launch_of(const MxProduct& p, dim3 grid, hipStream_t s) {
   if (p.epilogue == MX_GELU_CODES) mx_product_kernel<MT, 2, MX_GELU_CODES><<<grid, 256, 0, s>>>(p);
   else if (p.epilogue == MX_STORE_F32) mx_product_kernel<MT, 2, MX_STORE_F32><<<grid, 256, 0, s>>>(p);
   else mx_product_kernel<MT, 2, MX_STORE_BF16><<<grid, 256, 0, s>>>(p);
+}
+void launch_64(const MxProduct& p, dim3 grid, hipStream_t s) {
+  if (p.epilogue == MX_GELU_CODES) mx_product_kernel<2, 2, MX_GELU_CODES><<<grid, 256, 0, s>>>(p);
+  else if (p.epilogue == MX_STORE_F32) mx_product_kernel<2, 1, MX_STORE_F32><<<grid, 256, 0, s>>>(p);
+  else mx_product_kernel<2, 1, MX_STORE_BF16><<<grid, 256, 0, s>>>(p);
 }
 void launch_split(const MxProduct& p, dim3 grid, hipStream_t s) {
   if (p.epilogue == MX_GELU_CODES) mx_split_kernel<MX_GELU_CODES><<<grid, 256, 0, s>>>(p);
@@ -535,12 +544,21 @@ void launch_split(const MxProduct& p, dim3 grid, hipStream_t s) {
 
 }  // namespace
 
-// Rows per tile.  A tile of 128 rows reads its weights once for all of them, and one with fewer rows leaves out whole sub-tiles of 32; 32-row
-// tiles fill more of the chip.  Where the 128-row tiles (rows spread evenly over the groups) would be fewer than 128, half of the CUs: 32.  Measured
-// on both sides, us with 128 and 32 rows: 1024 dense rows 4096 -> 1024 (32 tiles) 15.6, 10.2; 2048 (64) 16.2, 11.5; 4096 (128) 17.2, 19.0;
-// 2048 rows 1024 -> 4096 (256) 10.8, 12.9; 8 groups of 250 rows 4096 -> 1024 (64) 19.2, 14.7; 1024 -> 4096 of 8 x 125 (128) 11.4, 11.5.
-// n_out: of the narrowest product that walks the tiles.
-int mx_tile_rows(int rows, int groups, int n_out) { return even_tiles(rows, groups, 128) * ((n_out + 255) / 256) < 128 ? 32 : 128; }
+// Rows per tile, from rows spread evenly over the groups.  What a CU takes in per 256 inputs: 48 KB for 128 rows x 256 columns, 24 KB for 64 x 128,
+// 36 KB for 32 x 256, at 64 bytes a clock.  us on both sides, two operands' sizes and rows each:
+// up to 32 rows a group: 32 (64 groups of 4, 1024 -> 4096 -> 1024: 59.1 with 128, 58.3 with 32; 256 groups of 2, 512 -> 1024 -> 512: 34.3, 32.7);
+// 128 from three quarters of the CUs on (4096 -> 1024: 4096 rows, 128 tiles: 16.3 with 128, 13.8 with 64; 8192, 256 tiles: 21.5, 22.5), but not for a
+// second round of few tiles unless the inputs are long (1024 -> 1024, 9216 rows, 288 tiles: 12.5, 11.9; 12288, 384: 12.6, 13.5; 4096 -> 1024,
+// 288: 28.2, 29.5); else 64 (2048 rows 4096 -> 1024: 10.8 with 32, 10.0 with 64; 200 rows 1024 -> 4096: 5.6, 4.4), where the inputs are not
+// split (500 rows 4096 -> 1024: 9.0 with 64, 7.5), and with the GELU epilogue, whose tiles keep 256 columns, only where there are enough
+// of them (FFN 256 -> 1024 -> 256, 8 groups of 125: 13.0 with 64, 12.0 with 32; 1536 -> 6144 -> 1536, 8 of 125: 32.3 with 32, 29.9 with 64).
+int mx_tile_rows(int rows, int groups, int n_in, int n_out, int epilogue) {
+  const long parts = (n_out + 255) / 256, tiles = even_tiles(rows, groups, 128) * parts;
+  if ((rows + groups - 1) / groups <= 32) return 32;
+  if (tiles >= 192 && (n_in >= 2048 || tiles <= 256 || tiles >= 384)) return 128;
+  if (worth_splitting(rows, groups, n_in, n_out)) return 32;
+  return epilogue == MX_GELU_CODES && even_tiles(rows, groups, 64) * parts < 256 ? 32 : 64;
+}
 
 int check_mx_product(const MxProduct& p) { return product_blocks(p) > MX_MAX_BLOCKS ? BIGMAC_ERR_TOO_LARGE : BIGMAC_OK; }
 
@@ -548,6 +566,7 @@ int launch_mx_product(const MxProduct& p, hipStream_t s) {
   const dim3 grid((unsigned)product_blocks(p));
   if (splits(p)) launch_split(p, grid, s);
   else if (p.tile_rows == 128) launch_of<4>(p, grid, s);
+  else if (p.tile_rows == 64) launch_64(p, grid, s);
   else launch_of<1>(p, grid, s);
   BIGMAC_CHECK_LAUNCH();
   return BIGMAC_OK;

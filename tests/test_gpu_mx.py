@@ -164,13 +164,14 @@ def test_dense_products(rows):
     check_product([rows], 576, 448, dense=True, bias=rows % 2 == 0, out="bf16" if rows > 64 else "f32")
 
 
-# groups enough that the tiles have 128 rows; row counts around every sub-tile's edge
+# row counts around every sub-tile's edge; groups for tiles of 64 rows and enough for tiles of 128
 EDGES = [0, 1, 31, 32, 33, 64, 65, 96, 97, 127, 128, 129, 200, 5, 0, 160]
 
 
 @pytest.mark.parametrize("n_in,n_out", [(64, 64), (320, 192), (1088, 64), (512, 320)])
-def test_tiles_of_128_rows(n_in, n_out):
-    counts = EDGES * 8
+@pytest.mark.parametrize("times", [8, 13])
+def test_tiles_of_64_and_128_rows(n_in, n_out, times):
+    counts = EDGES * times
     print(f"products of {sum(counts)} rows in {len(counts)} groups, {n_in} -> {n_out}", flush=True)
     check_product(counts, n_in, n_out, seed=n_in)
     check_product(counts, n_in, n_out, out="bf16", bias=True, spare=70, seed=n_in + 1)
@@ -276,6 +277,7 @@ class Ffn:
     (20, 1, 2, 2112, 64, [7, 13]),
     (12, 1, 2, 128, 2176, [0, 12]),
     (sum(EDGES) * 4, 2, 128, 192, 320, EDGES * 8),
+    (400, 2, 8, 128, 4096, [129, 64, 65, 63, 1, 0, 200, 278]),
 ], ids=lambda v: str(v)[:40])
 @pytest.mark.parametrize("bias", [False, True])
 def test_experts(T, k, N, r, h, counts, bias):
