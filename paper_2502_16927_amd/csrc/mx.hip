@@ -33,12 +33,16 @@ __device__ __forceinline__ void put8(bf16_t* p, const float* f) { *(uint4*)p = p
 // and the tiles are cut off at the most that ascending offsets make; the products leave out tiles outside their rows.
 __device__ __forceinline__ void build_mx_map(const MxMapJob& job) {
   __shared__ unsigned before[1025], wave_total[4];
+  __shared__ int start[1025];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g0 = threadIdx.x * 4;
   unsigned count[4], sum = 0;
+  int edge[5];
+#pragma unroll
+  for (int i = 0; i < 5; ++i) edge[i] = job.offsets[min(g0 + i, job.groups)];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int g = g0 + i;
-    count[i] = g < job.groups ? (unsigned)max((long)job.offsets[g + 1] - job.offsets[g] + job.tile_rows - 1, 0l) / (unsigned)job.tile_rows : 0;
+    count[i] = g < job.groups ? (unsigned)max((long)edge[i + 1] - edge[i] + job.tile_rows - 1, 0l) / (unsigned)job.tile_rows : 0;
     sum += count[i];
   }
   unsigned upto = sum;
@@ -54,10 +58,12 @@ __device__ __forceinline__ void build_mx_map(const MxMapJob& job) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     before[g0 + i] = at;
+    start[g0 + i] = edge[i];
     at += count[i];
   }
   if (threadIdx.x == 255) {
     before[1024] = min(at, (unsigned)mx_most_tiles(job.rows, job.groups, job.tile_rows));
+    start[1024] = edge[4];
     job.map[0] = (int)before[1024];
   }
   __syncthreads();
@@ -69,7 +75,7 @@ __device__ __forceinline__ void build_mx_map(const MxMapJob& job) {
       if (before[mid] <= i) lo = mid;
       else hi = mid;
     }
-    *(int2*)(job.map + 2 + 2 * i) = make_int2(lo, (int)((unsigned)job.offsets[lo] + (i - before[lo]) * (unsigned)job.tile_rows));
+    *(int4*)(job.map + 4 + 4 * (size_t)i) = make_int4(lo, (int)((unsigned)start[lo] + (i - before[lo]) * (unsigned)job.tile_rows), min(start[lo + 1], job.rows), 0);
   }
 }
 __global__ __launch_bounds__(256) void mx_map_kernel(MxMapJob job) { build_mx_map(job); }

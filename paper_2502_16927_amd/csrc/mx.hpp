@@ -69,7 +69,7 @@ struct MxProduct {
 int mx_tile_rows(int rows, int groups, int n_in, int n_out, int epilogue);   // 32, 64 or 128
 int check_mx_product(const MxProduct& p);   // BIGMAC_ERR_TOO_LARGE where its launch would be; before anything is launched
 int launch_mx_product(const MxProduct& p, hipStream_t s);
-// The row tiles of a ragged product: map[0] = how many, then from map[2] on (group, first row) of each, groups in order
+// The row tiles of a ragged product: map[0] = how many, then from map[4] on (group, first row, end of the group's rows, 0) of each, groups in order
 struct MxMapJob {
   const int* offsets;              // device [groups + 1]
   int* map;                        // device, mx_map_ints(rows, groups); NULL: no job
@@ -77,7 +77,7 @@ struct MxMapJob {
 };
 // upper bound of the row tiles (ascending offsets keep it by themselves, others are cut off at it)
 inline __host__ __device__ long mx_most_tiles(long rows, long groups, int tile_rows) { return rows / tile_rows + (groups < rows ? groups : rows); }
-inline size_t mx_map_ints(long rows, long groups) { return 2 + 2 * ((size_t)rows / 32 + groups + 1); }   // for every tile height
+inline size_t mx_map_ints(long rows, long groups) { return 4 + 4 * ((size_t)rows / 32 + groups + 1); }   // for every tile height
 // maps (optional): one or two tile maps, by workgroups of the same launch
 int launch_mx_quantize(long rows, long cols, int dtype, const void* src, uint8_t* codes, uint8_t* scales, hipStream_t s, const MxMapJob* maps = nullptr);
 
