@@ -189,13 +189,23 @@ def _ptr(t):
     return t.data_ptr()
 
 
+def _on(t, device=None):
+    """_ptr of a tensor on GPU `device` (None: on any): a launch on the current device takes no other device's memory, nor the host's."""
+    if t is None or isinstance(t, int):
+        return t
+    where = t.get_device()
+    if where < 0 or (device is not None and where != device):
+        raise ValueError(f"a tensor on {t.device}: the call's tensors lie on the current GPU" + ("" if device is None else f", {device}"))
+    return _ptr(t)
+
+
 def _nbytes(t):
     return 0 if t is None else t.numel() * t.element_size()
 
 
-def _stream(stream):
+def _stream(stream, device=None):
     if stream is None:      # the current stream's handle without a Stream object around it (2 us of a 7 us call)
-        stream = torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        stream = torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if device is None else device)
     return stream
 
 
@@ -267,7 +277,7 @@ def make_norm_dims(T, d, x_dtype=BF16, y_dtype=BF16, u_dtype=BF16, kind=NORM_RMS
 
 
 def make_norm_params(post_w=None, post_b=None, pre_w=None, pre_b=None, gate=None) -> NormParams:
-    return NormParams(_ptr(post_w), _ptr(post_b), _ptr(pre_w), _ptr(pre_b), _ptr(gate))
+    return NormParams(_on(post_w), _on(post_b), _on(pre_w), _on(pre_b), _on(gate))
 
 
 def norm_workspace_bytes(dims: NormDims) -> int:
@@ -275,12 +285,14 @@ def norm_workspace_bytes(dims: NormDims) -> int:
 
 
 def bigmac_norm_forward(dims, params, x, y, z, u, stream=None):
-    _check(lib().bigmac_norm_forward(ctypes.byref(dims), ctypes.byref(params), _ptr(x), _ptr(y), _ptr(z), _ptr(u), _stream(stream)), "bigmac_norm_forward")
+    at = torch.cuda.current_device()
+    _check(lib().bigmac_norm_forward(ctypes.byref(dims), ctypes.byref(params), _on(x, at), _on(y, at), _on(z, at), _on(u, at), _stream(stream, at)), "bigmac_norm_forward")
 
 
 def bigmac_norm_backward(dims, params, z, y, du, dz, dx, dy, d_gate, d_post_w, d_post_b, d_pre_w, d_pre_b, ws, stream=None):
-    _check(lib().bigmac_norm_backward(ctypes.byref(dims), ctypes.byref(params), _ptr(z), _ptr(y), _ptr(du), _ptr(dz), _ptr(dx), _ptr(dy), _ptr(d_gate),
-                                      _ptr(d_post_w), _ptr(d_post_b), _ptr(d_pre_w), _ptr(d_pre_b), _ptr(ws), _nbytes(ws), _stream(stream)),
+    at = torch.cuda.current_device()
+    _check(lib().bigmac_norm_backward(ctypes.byref(dims), ctypes.byref(params), _on(z, at), _on(y, at), _on(du, at), _on(dz, at), _on(dx, at), _on(dy, at), _on(d_gate, at),
+                                      _on(d_post_w, at), _on(d_post_b, at), _on(d_pre_w, at), _on(d_pre_b, at), _on(ws, at), _nbytes(ws), _stream(stream, at)),
            "bigmac_norm_backward")
 
 
@@ -301,29 +313,35 @@ def mx_workspace_bytes(dims: MxDims) -> int:
 
 
 def bigmac_mx_quantize(rows, cols, dtype, src, codes, scales, stream=None):
-    _check(lib().bigmac_mx_quantize(rows, cols, dtype, _ptr(src), _ptr(codes), _ptr(scales), _stream(stream)), "bigmac_mx_quantize")
+    at = torch.cuda.current_device()
+    _check(lib().bigmac_mx_quantize(rows, cols, dtype, _on(src, at), _on(codes, at), _on(scales, at), _stream(stream, at)), "bigmac_mx_quantize")
 
 
 def bigmac_mx_dequantize(rows, cols, codes, scales, dtype, dst, stream=None):
-    _check(lib().bigmac_mx_dequantize(rows, cols, _ptr(codes), _ptr(scales), dtype, _ptr(dst), _stream(stream)), "bigmac_mx_dequantize")
+    at = torch.cuda.current_device()
+    _check(lib().bigmac_mx_dequantize(rows, cols, _on(codes, at), _on(scales, at), dtype, _on(dst, at), _stream(stream, at)), "bigmac_mx_dequantize")
 
 
 def bigmac_mx_pack(groups, n_in, n_out, dtype, w, packed, stream=None):
-    _check(lib().bigmac_mx_pack(groups, n_in, n_out, dtype, _ptr(w), _ptr(packed), _stream(stream)), "bigmac_mx_pack")
+    at = torch.cuda.current_device()
+    _check(lib().bigmac_mx_pack(groups, n_in, n_out, dtype, _on(w, at), _on(packed, at), _stream(stream, at)), "bigmac_mx_pack")
 
 
 def bigmac_mx_unpack(groups, n_in, n_out, packed, dtype, w, stream=None):
-    _check(lib().bigmac_mx_unpack(groups, n_in, n_out, _ptr(packed), dtype, _ptr(w), _stream(stream)), "bigmac_mx_unpack")
+    at = torch.cuda.current_device()
+    _check(lib().bigmac_mx_unpack(groups, n_in, n_out, _on(packed, at), dtype, _on(w, at), _stream(stream, at)), "bigmac_mx_unpack")
 
 
 def bigmac_mx_product(dims, codes, scales, offsets, packed, bias, out, ws=None, stream=None):
-    _check(lib().bigmac_mx_product(ctypes.byref(dims), _ptr(codes), _ptr(scales), _ptr(offsets), _ptr(packed), _ptr(bias), _ptr(out), _ptr(ws), _nbytes(ws),
-                                   _stream(stream)), "bigmac_mx_product")
+    at = torch.cuda.current_device()
+    _check(lib().bigmac_mx_product(ctypes.byref(dims), _on(codes, at), _on(scales, at), _on(offsets, at), _on(packed, at), _on(bias, at), _on(out, at), _on(ws, at), _nbytes(ws),
+                                   _stream(stream, at)), "bigmac_mx_product")
 
 
 def bigmac_mx_grouped_ffn(dims, x_perm, expert_offsets, w1, w2, o_perm, ws, b1=None, b2=None, stream=None):
-    _check(lib().bigmac_mx_grouped_ffn(ctypes.byref(dims), _ptr(x_perm), _ptr(expert_offsets), _ptr(w1), _ptr(w2), _ptr(b1), _ptr(b2), _ptr(o_perm), _ptr(ws),
-                                       _nbytes(ws), _stream(stream)), "bigmac_mx_grouped_ffn")
+    at = torch.cuda.current_device()
+    _check(lib().bigmac_mx_grouped_ffn(ctypes.byref(dims), _on(x_perm, at), _on(expert_offsets, at), _on(w1, at), _on(w2, at), _on(b1, at), _on(b2, at), _on(o_perm, at), _on(ws, at),
+                                       _nbytes(ws), _stream(stream, at)), "bigmac_mx_grouped_ffn")
 
 
 def dispatch_folding(dims, training: bool) -> int:

@@ -3,6 +3,7 @@ import ctypes
 
 import numpy as np
 import pytest
+import torch
 
 from paper_2502_16927_amd import binding as B
 import block_reference as R
@@ -72,3 +73,26 @@ def test_sizes_and_refusals():
 @pytest.mark.parametrize("kind", range(8))
 def test_workspace_kinds_of_bad_dims(kind):
     assert B.workspace_bytes(B.make_dims(0, 128, 64, 8, 2, 128), kind) == 0
+
+
+def test_tensors_of_the_host_and_of_another_gpu_are_refused(monkeypatch):
+    """Before anything reaches the library: host tensors, and tensors of a GPU that is not the current one."""
+    class On1:
+        device = "cuda:1"
+
+        def get_device(self):
+            return 1
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    t, d = torch.zeros(64, dtype=torch.uint8), B.make_mx_dims(1, 1, 64, 64)
+    ffn, norm = B.make_dims(1, 64, 64, 1, 1, 64), B.make_norm_dims(1, 64)
+    with pytest.raises(ValueError):
+        B.make_norm_params(pre_w=torch.ones(64))
+    p = B.make_norm_params()
+    for bad in (t, On1()):
+        for call in (lambda: B.bigmac_mx_quantize(1, 64, B.BF16, bad, None, None), lambda: B.bigmac_mx_dequantize(1, 64, None, bad, B.F32, None),
+                     lambda: B.bigmac_mx_pack(1, 64, 64, B.BF16, None, bad), lambda: B.bigmac_mx_unpack(1, 64, 64, bad, B.BF16, None),
+                     lambda: B.bigmac_mx_product(d, None, None, None, bad, None, None), lambda: B.bigmac_mx_grouped_ffn(ffn, None, None, None, None, None, None, b2=bad),
+                     lambda: B.bigmac_norm_forward(norm, p, None, None, None, bad), lambda: B.bigmac_norm_backward(norm, p, *[None] * 11, bad)):
+            with pytest.raises(ValueError):
+                call()
