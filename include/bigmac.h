@@ -388,8 +388,9 @@ size_t bigmac_mx_workspace_bytes(const bigmac_mx_dims *dims); /* host only; 0 fo
 int bigmac_mx_product(const bigmac_mx_dims *dims, const void *codes, const void *scales, const int32_t *offsets, const void *packed,
                       const void *bias, void *out, void *ws, size_t ws_bytes, void *stream);
 
-/* bigmac_grouped_ffn with the experts' matrices in 4 bits: the rows of x_perm are quantised, multiplied by w1, then bias, activation (fp32),
- * the hidden rows quantised from fp32 (blocks whose scale would be under 2^-126: with that), multiplied by w2, bias, o_perm in bf16.  dtype BIGMAC_BF16 only (BIGMAC_ERR_UNSUPPORTED); w1 packed
+/* bigmac_grouped_ffn with the experts' matrices in 4 bits: the rows of x_perm are quantised, multiplied by w1, then bias, activation (within 2^-15 of the
+ * largest of the 32 values that share a scale), the hidden rows quantised from fp32 (blocks whose scale would be under 2^-126: with that), multiplied by
+ * w2, bias, o_perm in bf16.  dtype BIGMAC_BF16 only (BIGMAC_ERR_UNSUPPORTED); w1 packed
  * [N, win, hid], w2 packed [N, hid, win]; b1, b2 as there.  ws: BIGMAC_WS_MX_GROUPED_FFN.  Rows at or past expert_offsets[N] of o_perm
  * are left as they were. */
 int bigmac_mx_grouped_ffn(const bigmac_dims *dims, const void *x_perm, const int32_t *expert_offsets, const void *w1, const void *w2,

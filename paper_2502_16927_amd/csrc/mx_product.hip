@@ -32,8 +32,9 @@ template <int OFFSET>
 __device__ __forceinline__ void lds_read_b32(unsigned addr, unsigned& v) { asm volatile("ds_read_b32 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(OFFSET) : "memory"); }
 
 // GELU for 4-bit results: a polynomial of degree 5 for log2 of the normal tail (minimax of the tail's absolute error, of |a| times it past
-// 1: under 7e-7, so within 7e-7 of |a| and of 1; the smallest step of a 4-bit value is an eighth of it or more).  It falls without end, so |a|
-// needs no limit.  max(a, 0) on the bits as an integer: one instruction.  The vector ALU is what bounds a product with this epilogue: for
+// 1: under 7e-7, so within 7e-7 of |a| and of 1).  That is 2^-15 of a block's largest value where this is 2^-5 or more; smaller blocks with an input past 1,
+// which may hold the far tail alone (18 % off at -6), take gelu_tail_f (inputs up to 1: 2^-17 of the result).  The polynomial falls without end, so
+// |a| needs no limit.  max(a, 0) on the bits as an integer: one instruction.  The vector ALU is what bounds a product with this epilogue: for
 // the 131072 x 4096 hidden values of a 16384-token call every instruction per value is 16 us, and a matrix instruction leaves it about half of its time.
 __device__ __forceinline__ float gelu_mx_f(float a) {
   const float x = fabsf(a);
@@ -43,6 +44,22 @@ __device__ __forceinline__ float gelu_mx_f(float a) {
   q = fmaf(x, q, -1.151052049e+00f);
   q = fmaf(x, q, -1.000001856e+00f);
   return fmaf(-x, __builtin_amdgcn_exp2f(q), __int_as_float(max(__float_as_int(a), 0)));
+}
+// GELU for blocks of small values: e^(a^2 / 2) times the tail as t times a polynomial of degree 7 in t = 1 / (1 + 0.3 |a|) (minimax of the relative
+// error, 1.7e-7; with the roundings of a^2 and of the exponential within 1e-5 of the result down to 2^-124).  2^32 keeps the exponential of the
+// far tail from being flushed to 0.
+constexpr unsigned MX_GELU_SMALL = 0x3D000000u, MX_GELU_NEAR = 0x3F800000u;   // 2^-5 and 1, by their bits
+__device__ __forceinline__ float gelu_tail_f(float a) {
+  const float x = fabsf(a), t = __builtin_amdgcn_rcpf(fmaf(x, 0.3f, 1.0f));
+  float q = fmaf(t, 3.542370350e-02f, -1.561583233e-01f);
+  q = fmaf(t, q, 2.045565844e-01f);
+  q = fmaf(t, q, -5.203384629e-02f);
+  q = fmaf(t, q, 1.276916891e-01f);
+  q = fmaf(t, q, 1.001759707e-01f);
+  q = fmaf(t, q, 1.207121328e-01f);
+  q = fmaf(t, q, 1.196320074e-01f);
+  const float e = __builtin_amdgcn_exp2f(fmaf(x * -0.72134752f, x, 32.0f));
+  return fmaf(-(q * t * x * e), 0x1p-32f, __int_as_float(max(__float_as_int(a), 0)));
 }
 // largest magnitude of 16 values, NaN if one is
 __device__ __forceinline__ float top_of(const float (&f)[16]) {
@@ -143,32 +160,88 @@ __device__ __forceinline__ void mx_store(const MxProduct& p, const f32x16_t (&ac
     strip_out(strip, p, row0, rows, (size_t)(col0 + 32 * j) * 4, (size_t)p.n_out * 4, lane);
   }
 }
-// GELU and 4 bits of 32 rows x 64 columns: a block of a row per lane, the first 32 columns in the lower lanes; bytes: both blocks' scales
-template <int NS>
-__device__ __forceinline__ uint4 mx_gelu_blocks(const f32x16_t (&acc)[NS], const float (&bias)[NS][16], bool biased, unsigned (&bytes)[NS]) {
+// GELU and 4 bits of 32 rows x 64 columns: a block of a row per lane, the first 32 columns in the lower lanes; bytes: both blocks' scales.
+// TAIL false: every block by gelu_mx_f; small: whether a block of this lane's may need the other form (its row, `live`, is one of the tile's: the
+// others' values count for nothing).  TAIL true: the blocks that need it by gelu_tail_f.  Which form a block has depends on its own values only.
+template <int NS, bool TAIL>
+__device__ __forceinline__ uint4 mx_gelu_blocks(const f32x16_t (&acc)[NS], const float (&bias)[NS][16], bool biased, bool live, bool& small, unsigned (&bytes)[NS]) {
   static_assert(NS == 2, "a lane for each block");
   uint2 half_block[NS];   // lower lane: columns 0 .. 15 of a block, upper lane: 16 .. 31
+  unsigned least = ~0u;
 #pragma unroll
   for (int j = 0; j < NS; ++j) {
     float f[16];
+    auto inputs = [&]() {
 #pragma unroll
-    for (int v = 0; v < 16; ++v) f[v] = acc[j][v];
-    if (biased)
+      for (int v = 0; v < 16; ++v) f[v] = acc[j][v];
+      if (biased)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) f[v] += bias[j][v];
+        for (int v = 0; v < 16; ++v) f[v] += bias[j][v];
+    };
+    auto block_top = [&]() {   // bits of the largest magnitude (a NaN is the largest, with its sign or without)
+      const unsigned mine = __float_as_uint(top_of(f));
+      const auto both = __builtin_amdgcn_permlane32_swap(mine, mine, false, false);
+      return max(both[0], both[1]) & 0x7FFFFFFFu;
+    };
+    inputs();
+    const unsigned top_input = TAIL ? block_top() : 0u;   // (of sums that an addition has read: assembly reads no matrix instruction's result)
 #pragma unroll
     for (int v = 0; v < 16; ++v) f[v] = gelu_mx_f(f[v]);
-    const unsigned mine = __float_as_uint(top_of(f));
-    const auto both = __builtin_amdgcn_permlane32_swap(mine, mine, false, false);
+    unsigned top = block_top();
+    if constexpr (TAIL) {
+      if (top < MX_GELU_SMALL && top_input > MX_GELU_NEAR) {   // (both lanes of a block or none)
+        inputs();
+#pragma unroll
+        for (int v = 0; v < 16; ++v) f[v] = gelu_tail_f(f[v]);
+        top = block_top();
+      }
+    }
+    least = min(least, top);
     // the smallest scale here is 2^-126: values of a block under 2^-124 that 2^-127 would hold better
-    bytes[j] = max(mx_scale_byte(max(both[0], both[1]) & 0x7FFFFFFFu), 1u);   // (a NaN is the largest, with its sign or without)
+    bytes[j] = max(mx_scale_byte(top), 1u);
     // halfword q: this lane's four columns of quad q; lower lane: the lower and the upper lane's of quads 0 and 1, upper lane: of quads 2 and 3
     const auto r = __builtin_amdgcn_permlane32_swap(mx_codes8_scaled(f, bytes[j]), mx_codes8_scaled(f + 8, bytes[j]), false, false);
     half_block[j] = make_uint2((r[0] & 0xFFFFu) | (r[1] << 16), (r[0] >> 16) | (r[1] & 0xFFFF0000u));
   }
+  if constexpr (!TAIL) small |= live && least < MX_GELU_SMALL;
   const auto x = __builtin_amdgcn_permlane32_swap(half_block[0].x, half_block[1].x, false, false);
   const auto y = __builtin_amdgcn_permlane32_swap(half_block[0].y, half_block[1].y, false, false);
   return make_uint4(x[0], y[0], x[1], y[1]);
+}
+// GELU and 4 bits of MT x 32 rows x 64 columns, `put` stores a sub-tile's blocks.  First every block by the short form; then, in wavefronts with a
+// small block that has an input past 1, all over again with the other form where it is needed.  (Decided block by block on the way the branches
+// between the blocks cost 14 us of a 16384-token call; so it is 4.)
+template <int MT, int NS, typename Put>
+__device__ __forceinline__ void mx_gelu_tile(f32x16_t (&acc)[MT][NS], const float (&bias)[NS][16], bool biased, int rows, int lane, Put&& put) {
+  bool small = false;
+  unsigned bytes[NS];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+    if (i * 32 < rows) {
+      const uint4 block = mx_gelu_blocks<NS, false>(acc[i], bias, biased, i * 32 + (lane & 31) < rows, small, bytes);
+      put(i, block, bytes);
+    }
+  if (__builtin_expect(__any(small), 0)) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int j = 0; j < NS; ++j) hold(acc[i][j]);   // (or the compiler keeps every value of the first pass, out of registers)
+    float top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int j = 0; j < NS; ++j)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) top = fmaxf(top, fabsf(acc[i][j][v] + bias[j][v]));
+    if (__any(top > 1.0f)) {
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+        if (i * 32 < rows) {
+          const uint4 block = mx_gelu_blocks<NS, true>(acc[i], bias, true, true, small, bytes);   // (without biases: zeros)
+          put(i, block, bytes);
+        }
+    }
+  }
 }
 // biases of the columns a lane holds of the 32 NS from `strip` on (bias NULL: zeros)
 template <int NS>
@@ -374,15 +447,11 @@ __device__ __forceinline__ void mx_tile_product(const MxProduct& p, const MxTile
   float bias[NS][16];
   mx_bias<NS>(p, t, there ? strip0 : t.strip0, bias, lane);
   if constexpr (EPI == MX_GELU_CODES) {
-    if (there) {
-#pragma unroll
-      for (int i = 0; i < MT; ++i)
-        if (i * 32 < t.m_rows) {
-          unsigned bytes[NS];
-          *(uint4*)((char*)staging + piece_place(i * 32 + (lane & 31), wave * 2 + (lane >> 5))) = mx_gelu_blocks<NS>(acc[i], bias, p.bias != nullptr, bytes);
-          out_scales[(i * 32 + (lane & 31)) * 8 + (lane >> 5) * 4 + wave] = (uint8_t)(lane < 32 ? bytes[0] : bytes[1]);   // blocks 2 wave and 2 wave + 1: see mx.hpp
-        }
-    }
+    if (there)
+      mx_gelu_tile<MT, NS>(acc, bias, p.bias != nullptr, t.m_rows, lane, [&](int i, const uint4& block, const unsigned (&bytes)[NS]) {
+        *(uint4*)((char*)staging + piece_place(i * 32 + (lane & 31), wave * 2 + (lane >> 5))) = block;
+        out_scales[(i * 32 + (lane & 31)) * 8 + (lane >> 5) * 4 + wave] = (uint8_t)(lane < 32 ? bytes[0] : bytes[1]);   // blocks 2 wave and 2 wave + 1: see mx.hpp
+      });
     __syncthreads();
     const size_t row_out = (size_t)p.n_out / 2;
     const int pieces = min(8, strips - t.strip0);   // of the workgroup's 256 columns, 32 each
@@ -458,7 +527,7 @@ __global__ __launch_bounds__(256, 2) void mx_split_kernel(MxProduct p) {
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) c.a[ks] = __builtin_amdgcn_raw_buffer_load_b128(ba, a_off + (unsigned)chunk * 128u + ks * 32u, 0, 0);
   };
-  f32x16_t acc[NS];
+  f32x16_t accs[1][NS], (&acc)[NS] = accs[0];
 #pragma unroll
   for (int j = 0; j < NS; ++j) acc[j] = f32x16_t{0};
   const unsigned last_mask = steps & 3 ? (1u << (8 * (steps & 3))) - 1u : ~0u;   // (a scale byte of 255 there would make NaN of the weights' zeros)
@@ -498,13 +567,13 @@ __global__ __launch_bounds__(256, 2) void mx_split_kernel(MxProduct p) {
   float bias[NS][16];
   mx_bias<NS>(p, t, t.strip0, bias, lane);
   if constexpr (EPI == MX_GELU_CODES) {
-    unsigned bytes[NS];
-    const uint4 block = mx_gelu_blocks<NS>(acc, bias, p.bias != nullptr, bytes);
-    const int row = lane & 31, strip = t.strip0 + (lane >> 5);
-    if (row < t.m_rows) {
-      *(uint4*)((uint8_t*)p.out + (size_t)(t.m0 + row) * (p.n_out / 2) + (size_t)strip * 16) = block;
-      p.out_scales[mx_scale_at(p.rows, t.m0 + row, strip)] = (uint8_t)(lane < 32 ? bytes[0] : bytes[1]);
-    }
+    mx_gelu_tile<1, NS>(accs, bias, p.bias != nullptr, t.m_rows, lane, [&](int, const uint4& block, const unsigned (&bytes)[NS]) {
+      const int row = lane & 31, strip = t.strip0 + (lane >> 5);
+      if (row < t.m_rows) {
+        *(uint4*)((uint8_t*)p.out + (size_t)(t.m0 + row) * (p.n_out / 2) + (size_t)strip * 16) = block;
+        p.out_scales[mx_scale_at(p.rows, t.m0 + row, strip)] = (uint8_t)(lane < 32 ? bytes[0] : bytes[1]);
+      }
+    });
   } else {
     mx_store<NS>(p, acc, bias, t.m0, t.m_rows, t.strip0 * 32, (char*)staging, lane, std::integral_constant<int, EPI>{});
   }

@@ -315,3 +315,73 @@ def test_experts_on_another_stream_and_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(f.out, want), replay
+
+
+# ------------------------------------------------------------------ hidden blocks whose 32 inputs are all negative
+
+def ffn_limit(x, counts, w1, w2, b1):
+    """Like R.ffn with the activation held to include/bigmac.h: a hidden value is off by at most 2^-15 of the largest of its block, besides
+    what its input's own error makes of it (a product of n inputs adds 64 + n / 64 times in fp32, each off by 2 u of the partial sum at
+    most, and once for the bias; GELU taken at both ends of that, and inside 1.13 times it where the two ends enclose GELU's minimum)."""
+    outs, limits, at = [], [], 0
+    xq = R.quantise(x)[2]
+    for e, n in enumerate(counts):
+        a = xq[at:at + n]
+        pre, size = a @ w1[e] + b1[e], np.abs(a) @ np.abs(w1[e]) + np.abs(b1[e])
+        delta = 2 * (66 + a.shape[1] / 64) * R.U32 * size
+        h = R.gelu(pre)
+        off = np.maximum(np.abs(R.gelu(pre + delta) - h), np.abs(R.gelu(pre - delta) - h))
+        off = np.where(np.abs(pre + 0.7518) < 0.5, 1.13 * delta, off)
+        off = off + 2.0 ** -15 * np.repeat(np.abs(h).reshape(n, h.shape[1] // 32, 32).max(2), 32, 1)
+        q, sign = R.quantise(h)[2], np.where(h < 0, -1.0, 1.0)
+        moved = np.zeros_like(q)
+        for direction in (1.0, -1.0):
+            moved = np.maximum(moved, np.abs(R.quantise(sign * np.maximum(np.abs(h) + direction * off, 0.0))[2] - q))
+        want, osize = q @ w2[e], np.abs(q) @ np.abs(w2[e])
+        outs.append(want)
+        limits.append(2 * (65 + h.shape[1] / 64) * R.U32 * osize + R.HALF_STEP["bf16"] * np.abs(want) * (1 + 2.0 ** -10) + (1 + R.HALF_STEP["bf16"]) * (moved @ np.abs(w2[e])))
+        at += n
+    return np.concatenate(outs), np.concatenate(limits)
+
+
+# where the blocks' inputs lie: the tail out to where GELU leaves the range of 4-bit blocks' scales, the border between the two forms of the
+# activation (largest magnitude 2^-5: inputs about -2.25 or 0.061), blocks of tiny inputs beside far ones
+TAILS = [(-2.6, -2.0), (-3.5, -2.2), (-4.8, -4.2), (-5.5, -5.0), (-6.5, -6.0), (-7.5, -7.0), (-9.0, -8.5), (-12.3, -11.9), (0.04, 0.07), (-7.0, 1e-4), (-0.05, 0.05), (-1.0, 1.0)]
+
+
+@pytest.mark.parametrize("T,k,N,r,counts", [
+    (40, 2, 4, 128, [1, 31, 0, 40]),                                 # tiles of 32 rows
+    (20, 1, 1, 2112, [17]),                                          # inputs split over the wavefronts, rows behind the last
+    (1536, 2, 4, 192, [700, 801, 97, 1400]),                         # more rows: the larger tiles
+    (12288, 1, 2, 64, [5000, 7000]),
+], ids=["few", "split", "many", "more"])
+@pytest.mark.parametrize("bias", [True, False])
+def test_experts_with_hidden_blocks_of_the_tail(T, k, N, r, counts, bias):
+    """bias False: the same places by weights of an input that is 1 in every row, as 4 bits hold them."""
+    g = torch.Generator(device=DEV).manual_seed(r)
+    h = 32 * 2 * len(TAILS)                                          # an even and an odd block of every range
+    rand = lambda *shape: torch.randn(shape, generator=g, device=DEV)  # noqa: E731
+    lo, hi = (torch.tensor(v, device=DEV).repeat_interleave(2).repeat_interleave(32) for v in zip(*TAILS))
+    b1 = (lo + (hi - lo) * torch.rand((N, h), generator=g, device=DEV)).to(torch.bfloat16)
+    x = rand(T * k, r).to(torch.bfloat16)
+    w1 = (rand(N, r, h) * (0.1 * (hi - lo) / r ** 0.5)).to(torch.bfloat16)
+    if not bias:
+        x[:, :32], x[:, 0], w1[:, :32] = 0.0, 1.0, 0.0
+        w1[:, 0] = b1
+        b1 = torch.from_numpy(held(w1)[:, 0]).to(torch.bfloat16).to(DEV)
+    # every block's hidden values count alike in the output
+    weight = 1.0 / torch.from_numpy(np.abs(R.gelu(up(b1))).reshape(N, -1, 32).max(2)).to(DEV).repeat_interleave(32, 1)
+    w2 = (rand(N, h, r) * weight[:, :, None]).to(torch.bfloat16)
+    dims = B.make_dims(T, 4 * r, r, N, k, h)
+    out = torch.full((T * k, r), 7.0, dtype=torch.bfloat16, device=DEV)
+    ws = torch.full((B.workspace_bytes(dims, B.WS_MX_GROUPED_FFN),), 0xEE, dtype=torch.uint8, device=DEV)
+    print(f"experts with tail blocks, T {T} k {k} N {N} r {r} h {h} {counts}, bias {bias}", flush=True)
+    B.bigmac_mx_grouped_ffn(dims, x, offsets_of(counts), pack(w1), pack(w2), out, ws, b1=b1 if bias else None)
+    rows = sum(counts)
+    want, limit = ffn_limit(up(x)[:rows], counts, held(w1), held(w2), up(b1) if bias else np.zeros((N, h)))
+    off = np.abs(up(out)[:rows] - want)
+    scale = np.sqrt(np.mean(want ** 2))
+    print(f"off at most {off.max() / scale:.2e} of the RMS, limits {limit.mean() / scale:.2e} in the mean", flush=True)
+    assert (off <= limit).all(), f"{int((off > limit).sum())} of {off.size} off, worst {np.nanmax(off / limit)} of the limit"
+    assert (out[rows:] == 7.0).all(), "rows behind the last expert"
+    assert np.mean(limit > 0.05 * scale) < 0.2
