@@ -38,6 +38,7 @@ class NormDims(ctypes.Structure):
 
 class NormParams(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("post_w", "post_b", "pre_w", "pre_b", "gate")]
+    device = None           # GPU of the tensors (None: bare pointers, or none at all)
 
 
 class MxDims(ctypes.Structure):
@@ -277,7 +278,19 @@ def make_norm_dims(T, d, x_dtype=BF16, y_dtype=BF16, u_dtype=BF16, kind=NORM_RMS
 
 
 def make_norm_params(post_w=None, post_b=None, pre_w=None, pre_b=None, gate=None) -> NormParams:
-    return NormParams(_on(post_w), _on(post_b), _on(pre_w), _on(pre_b), _on(gate))
+    tensors = (post_w, post_b, pre_w, pre_b, gate)
+    at = next((t.get_device() for t in tensors if t is not None and not isinstance(t, int)), None)
+    p = NormParams(*(_on(t, at) for t in tensors))
+    p.device = at
+    return p
+
+
+def _norm_device(params) -> int:
+    """The current GPU, which has to be the parameters' (make_norm_params) as well as that of the call's tensors (_on)."""
+    at = torch.cuda.current_device()
+    if params.device is not None and params.device != at:
+        raise ValueError(f"parameters on GPU {params.device}: they lie on the current GPU, {at}")
+    return at
 
 
 def norm_workspace_bytes(dims: NormDims) -> int:
@@ -285,12 +298,12 @@ def norm_workspace_bytes(dims: NormDims) -> int:
 
 
 def bigmac_norm_forward(dims, params, x, y, z, u, stream=None):
-    at = torch.cuda.current_device()
+    at = _norm_device(params)
     _check(lib().bigmac_norm_forward(ctypes.byref(dims), ctypes.byref(params), _on(x, at), _on(y, at), _on(z, at), _on(u, at), _stream(stream, at)), "bigmac_norm_forward")
 
 
 def bigmac_norm_backward(dims, params, z, y, du, dz, dx, dy, d_gate, d_post_w, d_post_b, d_pre_w, d_pre_b, ws, stream=None):
-    at = torch.cuda.current_device()
+    at = _norm_device(params)
     _check(lib().bigmac_norm_backward(ctypes.byref(dims), ctypes.byref(params), _on(z, at), _on(y, at), _on(du, at), _on(dz, at), _on(dx, at), _on(dy, at), _on(d_gate, at),
                                       _on(d_post_w, at), _on(d_post_b, at), _on(d_pre_w, at), _on(d_pre_b, at), _on(ws, at), _nbytes(ws), _stream(stream, at)),
            "bigmac_norm_backward")

@@ -91,3 +91,39 @@ def test_pointers_that_do_not_go_with_the_parts():
     none = dict(z=None, du=None, d_pre_w=None)
     assert backward(post, P(1, 0, 0, 0, 0), dz=None, **none) == -1   # nothing to differentiate
     assert backward(both, P(1, 1, 1, 0, 0)) == -1                    # a bias without its gradient
+
+
+class Weights:
+    """Stands for a contiguous tensor on a GPU."""
+
+    def __init__(self, gpu):
+        self.gpu, self.device = gpu, f"cuda:{gpu}"
+
+    def get_device(self):
+        return self.gpu
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return 4096
+
+
+@pytest.mark.parametrize("name", ["post_w", "post_b", "pre_w", "pre_b", "gate"])
+def test_parameters_of_another_gpu_are_refused(name, monkeypatch):
+    """Weights, biases and the gate lie on the GPU that is current when they are used, whichever was when they were put together."""
+    here = [0]
+    monkeypatch.setattr(B.torch.cuda, "current_device", lambda: here[0])
+    monkeypatch.setattr(B, "_stream", lambda stream, device=None: None)
+    p = B.make_norm_params(**{name: Weights(1)})
+    forward = lambda: B.bigmac_norm_forward(dims(), p, None, None, None, None)  # noqa: E731
+    backward = lambda: B.bigmac_norm_backward(dims(), p, *[None] * 12)  # noqa: E731
+    for call in (forward, backward):
+        with pytest.raises(ValueError):
+            call()
+    here[0] = 1
+    for call in (forward, backward):                                 # on to the library's own checks: there is no x
+        with pytest.raises(B.BigmacError):
+            call()
+    with pytest.raises(ValueError):
+        B.make_norm_params(**{"pre_w": Weights(0), "post_w": Weights(0), name: Weights(1)}, **({} if name.endswith("_b") else {"post_b": Weights(0)}))
