@@ -306,7 +306,7 @@ using namespace bigmac;
 
 extern "C" {
 
-size_t bigmac_mx_scale_bytes(int64_t cols) { return cols < 1 || cols > MAX_COLS ? 0 : mx_scale_bytes(cols); }
+size_t bigmac_mx_scale_bytes(int64_t cols) { return cols < 32 || cols % 32 || cols > MAX_COLS ? 0 : mx_scale_bytes(cols); }
 
 size_t bigmac_mx_packed_bytes(int32_t groups, int32_t n_in, int32_t n_out) {
   return check_weights(groups, n_in, n_out) == BIGMAC_OK ? mx_packed_bytes(groups, n_in, n_out) : 0;

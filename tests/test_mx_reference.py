@@ -96,3 +96,12 @@ def test_tensors_of_the_host_and_of_another_gpu_are_refused(monkeypatch):
                      lambda: B.bigmac_norm_forward(norm, p, None, None, None, bad), lambda: B.bigmac_norm_backward(norm, p, *[None] * 11, bad)):
             with pytest.raises(ValueError):
                 call()
+
+
+def test_sizes_of_columns_that_the_calls_refuse():
+    """A size query answers for what the calls take: 0 for columns that bigmac_mx_quantize refuses."""
+    fake = ctypes.c_void_p(4096)
+    for cols in (1, 5, 31, 33, 48, 255, (1 << 24) + 32, -32, 1 << 40):
+        assert B.mx_scale_bytes(cols) == 0, cols
+        assert B.lib().bigmac_mx_quantize(1, cols, B.BF16, fake, fake, fake, None) < 0
+    assert [B.mx_scale_bytes(c) for c in (32, 224, 8224, 1 << 24)] == [8, 8, 33 * 8, 1 << 19]
