@@ -284,6 +284,33 @@ FfnPlan plan_ffn(const bigmac_dims& D) {
   p.total = p.down_map + mx_map_bytes((int)rows, D.N);
   return p;
 }
+// A product as far as sizes go, for ragged rows or dense ones
+MxProduct product_of(const bigmac_mx_dims& D, const int32_t* offsets) {
+  MxProduct p{};
+  p.offsets = offsets;
+  p.rows = D.rows; p.groups = D.groups; p.n_in = D.n_in; p.n_out = D.n_out;
+  p.epilogue = D.out_dtype == BIGMAC_F32 ? MX_STORE_F32 : MX_STORE_BF16;
+  p.tile_rows = mx_tile_rows(D.rows, D.groups, D.n_in, D.n_out, p.epilogue);
+  return p;
+}
+constexpr int32_t SOME_OFFSETS = 0;   // its address: where only the sizes of a ragged product are asked for
+// The FFN's two products as far as sizes and offsets (not NULL) go, or the code of what is too large; before anything is launched
+int ffn_products(const bigmac_dims& D, const int32_t* offsets, MxProduct& up, MxProduct& down) {
+  const Widths W = widths(D);
+  int rc = check_weights(D.N, W.win, W.hid);
+  if (!rc) rc = check_rows((int64_t)D.T * D.k, W.win, BIGMAC_BF16);
+  if (rc) return rc;
+  up.n_in = W.win; up.n_out = W.hid; up.epilogue = MX_GELU_CODES;
+  down.n_in = W.hid; down.n_out = W.win; down.epilogue = MX_STORE_BF16;
+  for (MxProduct* p : {&up, &down}) {
+    p->offsets = offsets;
+    p->rows = D.T * D.k; p->groups = D.N;
+    p->tile_rows = mx_tile_rows(p->rows, p->groups, p->n_in, p->n_out, p->epilogue);
+    rc = check_mx_product(*p);
+    if (rc) return rc;
+  }
+  return BIGMAC_OK;
+}
 
 }  // namespace
 
@@ -298,7 +325,10 @@ int launch_mx_quantize(long rows, long cols, int dtype, const void* src, uint8_t
   return BIGMAC_OK;
 }
 
-size_t mx_ffn_ws_bytes(const bigmac_dims& D) { return plan_ffn(D).total; }
+size_t mx_ffn_ws_bytes(const bigmac_dims& D) {
+  MxProduct up{}, down{};
+  return ffn_products(D, &SOME_OFFSETS, up, down) == BIGMAC_OK ? plan_ffn(D).total : 0;
+}
 
 }  // namespace bigmac
 
@@ -355,7 +385,9 @@ int bigmac_mx_unpack(int32_t groups, int32_t n_in, int32_t n_out, const void* pa
   return BIGMAC_OK;
 }
 
-size_t bigmac_mx_workspace_bytes(const bigmac_mx_dims* D) { return check_mx(D) == BIGMAC_OK ? mx_map_bytes(D->rows, D->groups) : 0; }
+size_t bigmac_mx_workspace_bytes(const bigmac_mx_dims* D) {
+  return check_mx(D) == BIGMAC_OK && check_mx_product(product_of(*D, &SOME_OFFSETS)) == BIGMAC_OK ? mx_map_bytes(D->rows, D->groups) : 0;
+}
 
 int bigmac_mx_product(const bigmac_mx_dims* D, const void* codes, const void* scales, const int32_t* offsets, const void* packed, const void* bias, void* out,
                       void* ws, size_t ws_bytes, void* stream) {
@@ -364,16 +396,12 @@ int bigmac_mx_product(const bigmac_mx_dims* D, const void* codes, const void* sc
   if (!codes || !scales || !packed || !out || !aligned({codes, scales, packed, bias, out})) return BIGMAC_ERR_INVALID_ARG;
   if (!offsets && D->groups != 1) return BIGMAC_ERR_INVALID_ARG;
   hipStream_t s = (hipStream_t)stream;
-  MxProduct p{};
+  MxProduct p = product_of(*D, offsets);
   p.codes = (const uint8_t*)codes; p.scales = (const uint8_t*)scales; p.packed = (const uint8_t*)packed; p.bias = (const bf16_t*)bias;
   p.out = out;
-  p.rows = D->rows; p.groups = D->groups; p.n_in = D->n_in; p.n_out = D->n_out;
-  p.epilogue = D->out_dtype == BIGMAC_F32 ? MX_STORE_F32 : MX_STORE_BF16;
-  p.tile_rows = mx_tile_rows(D->rows, D->groups, D->n_in, D->n_out, p.epilogue);
   if (offsets) {
     if (!ws || !aligned({ws})) return BIGMAC_ERR_INVALID_ARG;
     if (ws_bytes < mx_map_bytes(D->rows, D->groups)) return BIGMAC_ERR_WORKSPACE;
-    p.offsets = offsets;
     p.tile_map = (const int*)ws;
   }
   rc = check_mx_product(p);
@@ -390,36 +418,25 @@ int bigmac_mx_grouped_ffn(const bigmac_dims* D, const void* x_perm, const int32_
   int rc = check_dims(D);
   if (rc) return rc;
   if (D->dtype != BIGMAC_BF16) return BIGMAC_ERR_UNSUPPORTED;
-  const Widths W = widths(*D);
-  rc = check_weights(D->N, W.win, W.hid);
-  if (!rc) rc = check_rows((int64_t)D->T * D->k, W.win, BIGMAC_BF16);
+  MxProduct up{}, down{};
+  if (!expert_offsets) return BIGMAC_ERR_INVALID_ARG;
+  rc = ffn_products(*D, expert_offsets, up, down);
   if (rc) return rc;
-  if (!x_perm || !expert_offsets || !w1 || !w2 || !o_perm || !ws || !aligned({x_perm, w1, w2, b1, b2, o_perm, ws})) return BIGMAC_ERR_INVALID_ARG;
+  if (!x_perm || !w1 || !w2 || !o_perm || !ws || !aligned({x_perm, w1, w2, b1, b2, o_perm, ws})) return BIGMAC_ERR_INVALID_ARG;
   const FfnPlan plan = plan_ffn(*D);
   if (ws_bytes < plan.total) return BIGMAC_ERR_WORKSPACE;
   hipStream_t s = (hipStream_t)stream;
-  const int rows = (int)((long)D->T * D->k);
+  const int rows = up.rows;
   uint8_t* base = (uint8_t*)ws;
-  MxProduct up{}, down{};
   up.codes = base + plan.x_codes; up.scales = base + plan.x_scales; up.packed = (const uint8_t*)w1; up.bias = (const bf16_t*)b1;
   up.out = base + plan.h_codes; up.out_scales = base + plan.h_scales;
-  up.n_in = W.win; up.n_out = W.hid; up.epilogue = MX_GELU_CODES;
   down.codes = base + plan.h_codes; down.scales = base + plan.h_scales; down.packed = (const uint8_t*)w2; down.bias = (const bf16_t*)b2;
   down.out = o_perm;
-  down.n_in = W.hid; down.n_out = W.win; down.epilogue = MX_STORE_BF16;
-  up.tile_rows = mx_tile_rows(rows, D->N, up.n_in, up.n_out, up.epilogue);
-  down.tile_rows = mx_tile_rows(rows, D->N, down.n_in, down.n_out, down.epilogue);
   MxMapJob maps[2] = {{expert_offsets, (int*)(base + plan.up_map), rows, D->N, up.tile_rows}, {}};
   if (down.tile_rows != up.tile_rows) maps[1] = {expert_offsets, (int*)(base + plan.down_map), rows, D->N, down.tile_rows};
   up.tile_map = maps[0].map;
   down.tile_map = maps[1].map ? maps[1].map : maps[0].map;
-  for (MxProduct* p : {&up, &down}) {
-    p->offsets = expert_offsets;
-    p->rows = rows; p->groups = D->N;
-    rc = check_mx_product(*p);
-    if (rc) return rc;
-  }
-  rc = launch_mx_quantize(rows, W.win, BIGMAC_BF16, x_perm, base + plan.x_codes, base + plan.x_scales, s, maps);
+  rc = launch_mx_quantize(rows, up.n_in, BIGMAC_BF16, x_perm, base + plan.x_codes, base + plan.x_scales, s, maps);
   if (!rc) rc = launch_mx_product(up, s);
   return rc ? rc : launch_mx_product(down, s);
 }

@@ -105,3 +105,23 @@ def test_sizes_of_columns_that_the_calls_refuse():
         assert B.mx_scale_bytes(cols) == 0, cols
         assert B.lib().bigmac_mx_quantize(1, cols, B.BF16, fake, fake, fake, None) < 0
     assert [B.mx_scale_bytes(c) for c in (32, 224, 8224, 1 << 24)] == [8, 8, 33 * 8, 1 << 19]
+
+
+def test_workspace_of_experts_that_the_call_refuses():
+    fake = ctypes.c_void_p(4096)
+    for d in (B.make_dims((1 << 28) + 1, 128, 64, 8, 4, 128), B.make_dims(4, 128, 64, 8, 4, (1 << 24) + 64), B.make_dims(4, (1 << 24) + 64, 64, 8, 4, 64, order=B.ORDER_CDAC),
+              B.make_dims(1 << 28, 256, 256, 8, 4, 128), B.make_dims(4, 128, 128, 1024, 4, 1 << 24)):
+        assert B.lib().bigmac_mx_grouped_ffn(ctypes.byref(d), fake, fake, fake, fake, None, None, fake, fake, 1 << 62, None) == -5
+        assert B.workspace_bytes(d, B.WS_MX_GROUPED_FFN) == 0
+    d = B.make_dims(1 << 22, 128, 64, 8, 4, 128)
+    rows, up = 1 << 24, lambda n: -(-n // 256) * 256                                       # noqa: E731
+    at_least = up(rows * 32) + up(rows * 8) + up(rows * 64) + up(rows * 8)
+    assert at_least < B.workspace_bytes(d, B.WS_MX_GROUPED_FFN) < at_least * 1.1
+
+
+def test_workspace_of_products_that_the_call_refuses():
+    fake = ctypes.c_void_p(4096)
+    for d in (B.make_mx_dims(1 << 30, 1, 64, 1 << 20), B.make_mx_dims(1 << 24, 1024, 64, 1 << 16), B.make_mx_dims((1 << 30) + 1, 4, 64, 64)):
+        assert B.lib().bigmac_mx_product(ctypes.byref(d), fake, fake, fake, fake, None, fake, fake, 1 << 62, None) == -5
+        assert B.mx_workspace_bytes(d) == 0
+    assert B.mx_workspace_bytes(B.make_mx_dims(1 << 30, 1024, 64, 64)) >= 16 * (1 << 30) // 128
