@@ -385,3 +385,34 @@ def test_experts_with_hidden_blocks_of_the_tail(T, k, N, r, counts, bias):
     assert (off <= limit).all(), f"{int((off > limit).sum())} of {off.size} off, worst {np.nanmax(off / limit)} of the limit"
     assert (out[rows:] == 7.0).all(), "rows behind the last expert"
     assert np.mean(limit > 0.05 * scale) < 0.2
+
+
+@pytest.mark.parametrize("ragged", [False, True])
+def test_product_of_rows_past_32_bit_offsets(ragged):
+    """16 GiB of rows, 4 GiB of their codes: the last ones against an exact product (small integers, every block's scale 1)."""
+    rows, n, n_in, n_out = (1 << 21) + 300, 200, 4096, 64
+    g = torch.Generator(device=DEV).manual_seed(12)
+    whole = torch.tensor([0.0, 1.0, 2.0, 3.0, 4.0, 6.0], device=DEV)
+    pick = lambda *shape: whole[torch.randint(0, 6, shape, generator=g, device=DEV)] * (torch.randint(0, 2, shape, generator=g, device=DEV) * 2 - 1)  # noqa: E731
+    x = torch.zeros((rows, n_in), dtype=torch.bfloat16, device=DEV)
+    x[-n:] = pick(n, n_in).to(torch.bfloat16)
+    x[:, ::32] = 6.0
+    w = pick(2 if ragged else 1, n_in, n_out)
+    w[:, ::32] = 4.0
+    codes = torch.empty((rows, n_in // 2), dtype=torch.uint8, device=DEV)
+    scales = torch.empty((B.mx_scale_bytes(n_in) // 8, rows, 8), dtype=torch.uint8, device=DEV)
+    print(f"product of {rows} rows", flush=True)
+    B.bigmac_mx_quantize(rows, n_in, B.BF16, x, codes, scales)
+    dims = B.make_mx_dims(rows, len(w), n_in, n_out, B.F32)
+    out = torch.empty((rows, n_out), device=DEV)
+    B.bigmac_mx_product(dims, codes, scales, offsets_of([rows - 77, 77]) if ragged else None, pack(w.to(torch.bfloat16)), None, out, B.alloc_bytes(B.mx_workspace_bytes(dims)))
+    first, last = w[0].double().cpu(), w[-1].double().cpu()
+    tail = x[-n:].double().cpu()
+    want = tail @ first
+    if ragged:
+        want[-77:] = tail[-77:] @ last
+    assert torch.equal(out[-n:].double().cpu(), want)
+    assert (out[:-n].double() == (6.0 * first[::32].sum(0)).to(DEV)).all()
+    back = torch.empty((rows, n_in), dtype=torch.bfloat16, device=DEV)
+    B.bigmac_mx_dequantize(rows, n_in, codes, scales, B.BF16, back)
+    assert torch.equal(back[-n:], x[-n:]) and torch.equal(back[1 << 20], x[1 << 20])

@@ -288,3 +288,45 @@ def test_graph_replays_equal_eager():
         torch.cuda.synchronize()
         for n, t in outs.items():
             assert torch.equal(t, want[n]), f"replay {replay}: {n}"
+
+
+def test_branch_and_backward_past_32_bit_offsets():
+    """5 GiB a tensor: the last rows, past every 32-bit byte offset, go forward through a branch and back like the same rows alone."""
+    d, T, n = 8192, 327681, 64
+    g = torch.Generator(device=DEV).manual_seed(2)
+    w = torch.rand((2, d), generator=g, device=DEV) + 0.5
+    p = B.make_norm_params(post_w=w[0], pre_w=w[1])
+
+    def tensor(rows, fill=None):
+        t = torch.empty((rows, d), dtype=torch.bfloat16, device=DEV)
+        if fill is not None:
+            t[:-n] = fill
+            t[-n:].normal_(0.0, 1.0, generator=g)
+        return t
+
+    x, y, du, dz = tensor(T, 1.0), tensor(T, 1.0), tensor(T, 0.0), tensor(T, 0.0)
+
+    def step(x, y, du, dz):
+        rows = x.shape[0]
+        dims = B.make_norm_dims(rows, d)
+        z, u, dx, dy = (tensor(rows) for _ in range(4))
+        vectors = torch.empty((2, d), device=DEV)
+        B.bigmac_norm_forward(dims, p, x, y, z, u)
+        B.bigmac_norm_backward(dims, p, z, y, du, dz, dx, dy, None, vectors[0], None, vectors[1], None, B.alloc_bytes(B.norm_workspace_bytes(dims)))
+        return z, u, dx, dy, vectors
+
+    print(f"norms of {T} rows", flush=True)
+    many, few = step(x, y, du, dz), step(*(t[-n:] for t in (x, y, du, dz)))
+    for name, a, b in zip(("z", "u", "dx", "dy"), many, few):
+        assert torch.equal(a[-n:], b), name
+    assert (many[2][:-n] == 0).all() and (many[3][:-n] == 0).all()
+    # the other rows add nothing; the sums of 64 rows in two orders are within 63 roundings each of the sum of magnitudes, which the values bound
+    off = (many[4].double() - few[4].double()).abs()
+    z, y64, du64, dz64 = (t.double() for t in (few[0], y[-n:], du[-n:], dz[-n:]))
+    unit = lambda v: v / (v.square().mean(1, keepdim=True) + 1e-5).sqrt()  # noqa: E731
+    pre = du64.abs() * unit(z).abs()
+    a = du64 * w[1].double()
+    dZ = dz64 + (a - unit(z) * (a * unit(z)).mean(1, keepdim=True)) / (z.square().mean(1, keepdim=True) + 1e-5).sqrt()
+    post = dZ.abs() * unit(y64).abs()
+    limit = torch.stack([post.sum(0), pre.sum(0)]) * 2 * 70 * R.U32
+    assert (off <= limit * 1.01).all()
