@@ -268,9 +268,10 @@ __device__ __forceinline__ void mx_bias(const MxProduct& p, const MxTile& t, int
 // to and chunk c + 2 is requested.  A chunk's step: the MT NS instructions of 64 inputs, between them the LDS reads of the next
 // step's fragments, behind them the next chunk's weights of the same step, into the registers that have just been read.
 //
-// What bounds it, at 131072 rows, 1024 -> 4096 with GELU and 4096 -> 1024 without (389 and 304 us, 280 with the scales of 256 columns together;
-// 2.8 and 3.9 PFLOP/s, matrix cores busy 31 and 39 % at 2.2 GHz): without the epilogues 259 and 270 us (53 % at 1.9 GHz), without the loop's requests too 190 (78 % at
-// 1.8 GHz), without its LDS reads too 160: power holds the clock down, and the requests cost as much as the epilogue.  Two workgroups share a CU.
+// At 131072 rows, 1024 -> 4096 with GELU and 4096 -> 1024 without, it takes 402 to 423 and 277 to 284 us in a call of the FFN (2.7 and 3.9 PFLOP/s).  What
+// bounds it, measured before the scales of 256 columns lay together, each product over and over (389 and 304 us, matrix cores busy 31 and 39 % at 2.2 GHz):
+// without the epilogues 259 and 270 us (53 % at 1.9 GHz), without the loop's requests too 190 (78 % at 1.8 GHz), without its LDS reads too 160: power holds the
+// clock down, and the requests cost as much as the epilogue.  Two workgroups share a CU.
 // Slower or level: one persistent workgroup walking many tiles with its operands requested a tile ahead (917 us a 16384-token call against 873),
 // 256 x 256 tiles by eight wavefronts (960 against 819), 64-row tiles (885 against 797), 32 columns a wavefront (888 against 874), weights two
 // chunks ahead (807 against 796), the rows of a tile kept in the LDS for all columns (803 against 799); for 32-row tiles weights two chunks ahead

@@ -8,7 +8,8 @@
 // What bounds them: HBM.  A row passes through registers once: a wavefront (up to 512 columns) or 2 to 16 of one workgroup hold it,
 // 8 columns a lane, so every tensor is read once and written once, and the statistics of the backward are worked out again from the
 // rows that it reads anyway instead of being stored.  (16 columns a lane: 154 registers forward, 234 backward, two wavefronts a SIMD.)  32768 rows
-// of 4096, bf16 stream, fp32 y: forward 242 us (5.6 TB/s), backward 428 us (5.0 TB/s; a large copy reaches 4.9).  Vectors (weights, channel
+// of 4096, bf16 stream, fp32 y: forward 242 us (5.6 TB/s), backward 428 us (5.0 TB/s; a large copy reaches 4.9, a sum of two tensors 6.05).  Wider rows
+// are slower: 16384 of 8192 252 and 672 us (5.3 and 3.2 TB/s, see the backward), 26208 of 5120, whose lanes are half idle, 345 and 940.  Vectors (weights, channel
 // gate) stay in registers over the rows of a persistent workgroup.  Sums and statistics are fp32; a layer norm's variance is
 // taken behind its mean.  Rows are addressed as buffers (range = the row): a lane past the end of the row loads zeros and its
 // stores are dropped, and the two halves of an fp32 piece and the one of a bf16 piece are the same code without a branch.
@@ -205,7 +206,9 @@ __global__ __launch_bounds__((RowShape<W>::THREADS)) void norm_forward_kernel(No
 }
 
 // Vectors of partial sums, in this order as far as the call has them: du z^, dn y^ (with a channel gate dZ y^), du, dn (dZ)
-// Four wavefronts a SIMD where the sums leave room: 32768 x 4096 471 -> 443 us; with biases their registers spill, 43 -> 50 us at 6001 x 1024.
+// Four wavefronts a SIMD without biases: 32768 x 4096 471 -> 443 us, although with both norms 10 registers spill there (1 with 4 wavefronts a row); with biases
+// too many would, 43 -> 50 us at 6001 x 1024.  16 wavefronts a row (past 4096 columns) are 1024 threads, 128 registers whatever is asked for: with both norms 56
+// spill, with biases 81, and 16384 x 8192 takes 672 and 845 us (3.2 and 2.5 TB/s).
 template <int W, bool POST, bool PRE, bool BIAS>
 __global__ __launch_bounds__((RowShape<W>::THREADS), BIAS ? 1 : 4) void norm_backward_kernel(NormArgs p) {
   using S = RowShape<W>;
