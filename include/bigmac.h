@@ -307,7 +307,8 @@ int bigmac_topk_folding(const bigmac_dims *dims, int training);
  *     n(v) = w (v - m) / sqrt(mean((v - m)^2) + eps) + b,   m = mean(v) (BIGMAC_NORM_LAYER) or 0 (BIGMAC_NORM_RMS)
  * With BIGMAC_NORM_PRE alone there is no branch: u = n_pre(x).  With BIGMAC_NORM_POST alone u is not made.
  * u is the norm of z as it is stored (rounded to x_dtype), so that the backward, which reads z, sees the same rows.
- * Statistics and sums are fp32; a layer norm's variance is taken behind its mean. */
+ * Statistics and sums are fp32; a layer norm's variance is taken behind its mean.  (So a row whose sum of squares passes fp32's range has no norm: rstd
+ * becomes 0.) */
 typedef enum { BIGMAC_NORM_RMS = 0, BIGMAC_NORM_LAYER = 1 } bigmac_norm_kind;
 typedef enum {
   BIGMAC_GATE_NONE = 0,    /* g = 1                                                              */

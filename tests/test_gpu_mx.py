@@ -416,3 +416,27 @@ def test_product_of_rows_past_32_bit_offsets(ragged):
     back = torch.empty((rows, n_in), dtype=torch.bfloat16, device=DEV)
     B.bigmac_mx_dequantize(rows, n_in, codes, scales, B.BF16, back)
     assert torch.equal(back[-n:], x[-n:]) and torch.equal(back[1 << 20], x[1 << 20])
+
+
+@pytest.mark.parametrize("T,r", [(24, 128), (20, 2112), (700, 128), (6000, 64)])
+def test_a_row_does_not_depend_on_its_neighbours_blocks(T, r):
+    """Rows beside others whose hidden blocks lie in GELU's tail: the same bits as beside others that do not."""
+    g = torch.Generator(device=DEV).manual_seed(T)
+    h = 320
+    x = torch.randn((T, r), generator=g, device=DEV).to(torch.bfloat16)
+    x[:, :32] = 0.0
+    w1 = (torch.randn((1, r, h), generator=g, device=DEV) / r ** 0.5).to(torch.bfloat16)
+    w1[:, :32] = 0.0
+    w1[:, 0] = -8.0
+    w2 = pack(torch.randn((1, h, r), generator=g, device=DEV).to(torch.bfloat16))
+    w1 = pack(w1)
+    dims = B.make_dims(T, 4 * r, r, 1, 1, h)
+    ws = B.alloc_bytes(B.workspace_bytes(dims, B.WS_MX_GROUPED_FFN))
+    outs = []
+    for deep in (False, True):
+        x[1::3, 0] = 1.0 if deep else 0.0
+        out = torch.empty((T, r), dtype=torch.bfloat16, device=DEV)
+        B.bigmac_mx_grouped_ffn(dims, x, offsets_of([T]), w1, w2, out, ws)
+        outs.append(out)
+    keep = [i for i in range(T) if i % 3 != 1]
+    assert torch.equal(outs[0][keep], outs[1][keep]) and not torch.equal(outs[0][1::3], outs[1][1::3])
